@@ -317,6 +317,83 @@ gqla_status gqla_expand_cache_fp8(const gqla_shape* shape, const gqla_cache* lat
                                   float v_scale, void* ws, size_t ws_bytes, void* stream);
 int64_t gqla_expanded_fp8_bytes_per_token(int32_t groups, int32_t d_h, int32_t d_r);
 
+/* ---- 8-bit expanded cache with a scale per block of tokens and group -------------------------------------------------
+ * The expanded cache again in E4M3 codes, scaled block by block, so that nothing has to be known of the values ahead of time: a
+ * block is 32 consecutive tokens (logical positions 32 i .. 32 i + 31) of one group, K and V apart, and its scale is 2^e with the
+ * smallest integer e for which the block's largest finite magnitude is at most 448 * 2^e, kept within -100 <= e <= 118:
+ *     code = E4M3(x * 2^-e)   round to nearest even; infinities and magnitudes beyond 448 * 2^e become +-448 * 2^e, NaN stays NaN
+ *     x'   = value(code) * 2^e   (exact in bf16)
+ * A page of P tokens and g_c groups (any (d_h, d_v) of the 16-bit expanded cache: (128, 128) or (192, 256)) has
+ * gqla_expanded_fp8_blocks_page_bytes = P * (g_c (d_h + d_v) + 2 d_r) + g_c (P / 32) * 8 BYTES (offsets inside the page):
+ *     K8    : [g_c][d_h/16][P][16]      dim d = 32 kp + 16 u + 8 h + i  ->  ((j*(d_h/16) + 2 kp + h)*P + s)*16 + 8 u + i
+ *     V8    : [g_c][P/32][d_v][2][16]   slot s = 32 T + 16 u + 8 h + i  ->  g_c*P*d_h + (((j*(P/32) + T)*d_v + d)*2 + h)*16 + 8 u + i
+ *     k_R   : [d_r/8][P][8] 16-bit      g_c*P*(d_h + d_v) + (((d/8)*P + s)*8 + d%8)*2
+ *     scales: [g_c][P/32][2] fp32       P*(g_c (d_h + d_v) + 2 d_r) + ((j*(P/32) + T)*2 + kind)*4, kind 0: K, 1: V; powers of two
+ * Shapes with GQLA_BF16 only (GQLA_ERR_DTYPE otherwise).
+ *
+ * gqla_quantize_expanded_fp8_blocks converts a 16-bit expanded cache (the groups it holds, every token t < L_b, L_b read from
+ * expanded->seq_lens on the device) into one with block scales, same page geometry; bytes of slots no token owns and scales
+ * of blocks no token owns are left as they are.  Errors as for gqla_quantize_expanded.
+ *
+ * gqla_decode_gqa_fp8_blocks is gqla_decode_gqa over such a cache: same plan, workspace, outputs and errors. */
+gqla_status gqla_quantize_expanded_fp8_blocks(const gqla_shape* shape, const gqla_cache* expanded, const gqla_cache* expanded_blocks,
+                                              void* stream);
+gqla_status gqla_decode_gqa_fp8_blocks(const gqla_shape* shape, const gqla_plan* plan, const void* q_c, const void* q_r,
+                                       const gqla_cache* expanded_blocks, void* out, float* lse, void* ws, size_t ws_bytes,
+                                       void* stream);
+/* 0 for sizes that no such page has (groups, dims or page_size not positive, page_size not a multiple of 32) */
+int64_t gqla_expanded_fp8_blocks_page_bytes(int32_t groups, int32_t d_h, int32_t d_v, int32_t d_r, int32_t page_size);
+
+/* ---- rows of new tokens into the expanded caches, with the rotation on the way -------------------------------------------
+ * Any number of new tokens per sequence: a step's one or two, a prompt, a chunk of one.  Rows are packed, sequence after sequence:
+ * rows first[b] .. first[b + 1] - 1 are the new tokens of sequence b (first: DEVICE memory, int32[batch + 1], not falling, at most
+ * `total`; with first = NULL every sequence has s_q rows and total must be batch * s_q).  Row i of a sequence with n of them
+ * is its token at position t = L_b - n + i, L_b read from expanded->seq_lens on the device (the lengths count the new
+ * tokens already, as everywhere); rows with t < 0 or beyond the page table's row are dropped, their q_r too where t < 0.  Rows that no sequence owns are not
+ * touched.  With L_b, first and the page table on the device and `total` an upper bound, one recorded graph serves any
+ * lengths up to the buffers' size. */
+typedef struct {
+  const void* k_c;       /* device [total][g][d_h]: the new tokens' K_C                                              */
+  const void* v;         /* device [total][g][d_v]                                                                   */
+  const void* k_r;       /* device [total][d_r], not rotated yet                                                     */
+  const void* q_r;       /* device [total][h_q][d_r], not rotated yet; or NULL                                        */
+  void* q_rot;           /* device [total][h_q][d_r]: receives the rotated q_r (may be q_r itself); NULL with it       */
+  const int32_t* first;  /* device int32[batch + 1], or NULL                                                         */
+  int64_t k_stride;      /* elements from one row of k_c, v, k_r to the next (parts of a joint projection's rows);     */
+  int64_t v_stride;      /*   0: rows follow each other; otherwise a multiple of 8 (GQLA_ERR_ALIGN) and not shorter than */
+  int64_t kr_stride;     /*   a row (GQLA_ERR_SHAPE)                                                                 */
+  int32_t total;         /* rows that the buffers hold                                                               */
+} gqla_new_rows;
+
+/* gqla_append_expanded writes the rows into an expanded cache of the shape's element type (16-bit or fp32),
+ * gqla_append_expanded_fp8_blocks into one with block scales.  K_C and V as they are, k_R turned by rope_t as in gqla_rope_step (rope_base
+ * finite and > 1; 0: copied without rotation, q_r too).  expanded->groups must be shape->g (a tensor-parallel slice passes a shape
+ * with h_q and g already divided).  Each page that receives rows belongs to one sequence.
+ * Block scales: a block that begins inside the new rows takes its exponent from them.  A block that holds older tokens keeps the
+ * larger of its own exponent and the one that the new rows need; where it grows, the older codes are rounded to the new
+ * scale (exact but for codes that fall below E4M3's normal range).  Appending the same rows again changes nothing.
+ * Errors: GQLA_ERR_SHAPE for another group count, rope_base, total < 0, total > 2^30, batch > 2^24, d_r odd or above 512; GQLA_ERR_NULL for q_r without
+ * q_rot or the reverse; others as for gqla_append_latent.  Both calls only enqueue one kernel on `stream`. */
+gqla_status gqla_append_expanded(const gqla_shape* shape, const gqla_new_rows* rows, float rope_base, const gqla_cache* expanded,
+                                 void* stream);
+gqla_status gqla_append_expanded_fp8_blocks(const gqla_shape* shape, const gqla_new_rows* rows, float rope_base,
+                                            const gqla_cache* expanded_blocks, void* stream);
+
+/* ---- attention of prompt chunks over the cache with block scales ------------------------------------------------------------
+ * The GQA-path equation (Sec. 3.1) for any number of query rows per sequence: rows packed as above (first, total), q_c
+ * [total][h_q][d_h] and q_r [total][h_q][d_r] (rotated), out [total][h_q][d_v], lse [total][h_q] fp32 or NULL.  Row i of a sequence
+ * with n of them sits at position t = L_b - n + i (L_b from expanded_blocks->seq_lens on the device, new tokens included and already
+ * appended) and sees tokens s <= t.  A row that sees nothing (t < 0, or only pages outside the pool) gets out = 0, lse = -inf; rows
+ * that no sequence owns are not touched.  A NaN among the values of a tile of 32 tokens reaches every row that has a token of the tile in sight.
+ * ws: device scratch of at least gqla_attend_gqa_workspace_bytes(shape, first, total, expanded_blocks) bytes, 16-byte aligned (fp32
+ * partial outputs over ranges of a long context, where there are few rows; may be NULL when that is 0).  It depends on the sizes
+ * only, max_pages * page_size standing for the longest context; its content is the call's own.
+ * Errors: GQLA_ERR_WORKSPACE when ws is missing or too small, GQLA_ERR_SHAPE when total * h_q / g or the launch exceeds 2^31; others as above. */
+gqla_status gqla_attend_gqa_fp8_blocks(const gqla_shape* shape, const int32_t* first, int32_t total, const void* q_c, const void* q_r,
+                                       const gqla_cache* expanded_blocks, void* out, float* lse, void* ws, size_t ws_bytes,
+                                       void* stream);
+size_t gqla_attend_gqa_workspace_bytes(const gqla_shape* shape, const int32_t* first, int32_t total, const gqla_cache* expanded_blocks);
+
 /* ---- 8-bit latent cache for the MQA-absorb path ----------------------------------------------------------
  * The same reading (Sec. 2; Sec. 5.1, item (i): quantised caches are complementary, no format given) applied to the
  * cache of Sec. 4.2.1: c_kv as E4M3 codes with ONE positive scale for the whole cache (conversion rule as above),
@@ -405,8 +482,8 @@ double gqla_probe_mfma_flops(int32_t iters, int32_t num_cus);
 
 /* Kernel timing (measurement only).  A decode call launches two kernels, the split-L decode kernel and the small
  * combine; events placed around the call time both.  After gqla_time_next_decode_kernel(event_begin, event_end) -- two
- * hipEvent_t created by the caller with timing enabled, passed as void* -- the NEXT gqla_decode_absorb, gqla_decode_gqa
- * or gqla_decode_gqa_fp8 call made by the same host thread records event_begin immediately before and event_end
+ * hipEvent_t created by the caller with timing enabled, passed as void* -- the NEXT gqla_decode_absorb, gqla_decode_gqa,
+ * gqla_decode_gqa_fp8 or gqla_decode_gqa_fp8_blocks call made by the same host thread records event_begin immediately before and event_end
  * immediately after its split-L decode kernel, on the call's stream; the pair is then forgotten (one call only; a call
  * that fails its argument checks still consumes it once it got past them).  Two NULLs forget a pending pair;
  * one NULL is GQLA_ERR_NULL.  The library keeps no reference to the events after that decode call returns. */

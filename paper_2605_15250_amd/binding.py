@@ -34,6 +34,8 @@ EXPORTS = [
     "gqla_expanded_elems_per_token_dv", "gqla_expanded_k_offset_dv", "gqla_expanded_v_offset_dv", "gqla_expanded_kr_offset_dv",
     "gqla_time_next_decode_kernel", "gqla_expand_cache_tail_static", "gqla_expand_cache_tail_static_max_workspace",
     "gqla_pack_expand_weights", "gqla_expand_cache_tail_packed",
+    "gqla_quantize_expanded_fp8_blocks", "gqla_decode_gqa_fp8_blocks", "gqla_expanded_fp8_blocks_page_bytes", "gqla_append_expanded",
+    "gqla_append_expanded_fp8_blocks", "gqla_attend_gqa_fp8_blocks", "gqla_attend_gqa_workspace_bytes",
 ]
 
 
@@ -51,6 +53,11 @@ class gqla_shape(C.Structure):
 class gqla_cache(C.Structure):
     _fields_ = [("pool", C.c_void_p), ("seq_lens", C.c_void_p), ("page_table", C.c_void_p), ("page_size", C.c_int32),
                 ("max_pages", C.c_int32), ("num_pages", C.c_int32), ("groups", C.c_int32)]
+
+
+class gqla_new_rows(C.Structure):
+    _fields_ = [("k_c", C.c_void_p), ("v", C.c_void_p), ("k_r", C.c_void_p), ("q_r", C.c_void_p), ("q_rot", C.c_void_p),
+                ("first", C.c_void_p), ("k_stride", C.c_int64), ("v_stride", C.c_int64), ("kr_stride", C.c_int64), ("total", C.c_int32)]
 
 
 class gqla_path_estimate(C.Structure):
@@ -137,6 +144,20 @@ def lib():
         L.gqla_latent_fp8_bytes_per_token.restype = i64
         L.gqla_expanded_fp8_bytes_per_token.argtypes = [i32, i32, i32]
         L.gqla_expanded_fp8_bytes_per_token.restype = i64
+        rp = C.POINTER(gqla_new_rows)
+        L.gqla_quantize_expanded_fp8_blocks.argtypes = [sp, cp, cp, vp]
+        L.gqla_quantize_expanded_fp8_blocks.restype = i32
+        L.gqla_decode_gqa_fp8_blocks.argtypes = [sp, vp, vp, vp, cp, vp, vp, vp, sz, vp]
+        L.gqla_decode_gqa_fp8_blocks.restype = i32
+        L.gqla_expanded_fp8_blocks_page_bytes.argtypes = [i32, i32, i32, i32, i32]
+        L.gqla_expanded_fp8_blocks_page_bytes.restype = i64
+        for name in ("gqla_append_expanded", "gqla_append_expanded_fp8_blocks"):
+            getattr(L, name).argtypes = [sp, rp, C.c_float, cp, vp]
+            getattr(L, name).restype = i32
+        L.gqla_attend_gqa_fp8_blocks.argtypes = [sp, vp, i32, vp, vp, cp, vp, vp, vp, sz, vp]
+        L.gqla_attend_gqa_fp8_blocks.restype = i32
+        L.gqla_attend_gqa_workspace_bytes.argtypes = [sp, vp, i32, cp]
+        L.gqla_attend_gqa_workspace_bytes.restype = sz
         L.gqla_probe_stream_read.argtypes = [vp, C.c_size_t, vp, i32, vp]
         L.gqla_probe_stream_read.restype = i32
         L.gqla_probe_mfma_bf16.argtypes = [vp, i32, i32, vp]
@@ -235,6 +256,11 @@ def make_shape(batch, h_q, g, d_h, r_kv, d_r, s_q, dtype, scale=0.0, d_v=0) -> g
 
 def make_cache(pool, seq_lens, page_table, page_size, max_pages, num_pages, groups=0) -> gqla_cache:
     return gqla_cache(_ptr(pool), _ptr(seq_lens), _ptr(page_table), page_size, max_pages, num_pages, groups)
+
+
+def make_new_rows(k_c, v, k_r, q_r=None, q_rot=None, first=None, total=0, k_stride=0, v_stride=0, kr_stride=0) -> gqla_new_rows:
+    """first: device int32[batch + 1] or None; strides in elements from row to row, 0 where rows follow each other."""
+    return gqla_new_rows(_ptr(k_c), _ptr(v), _ptr(k_r), _ptr(q_r), _ptr(q_rot), _ptr(first), k_stride, v_stride, kr_stride, total)
 
 
 # ---- plan -------------------------------------------------------------------------------------------------
@@ -400,6 +426,42 @@ def gqla_decode_gqa_fp8(shape, plan, q_c, q_r, expanded_fp8: gqla_cache, k_scale
     nbytes = ws_bytes if ws_bytes is not None else ws.numel() * ws.element_size()
     _check(lib().gqla_decode_gqa_fp8(C.byref(shape), plan, _ptr(q_c), _ptr(q_r), C.byref(expanded_fp8), float(k_scale),
                                      float(v_scale), _ptr(out), _ptr(lse), _ptr(ws), nbytes, _stream(stream)), "gqla_decode_gqa_fp8")
+
+
+def gqla_quantize_expanded_fp8_blocks(shape, expanded: gqla_cache, expanded_blocks: gqla_cache, stream=None):
+    _check(lib().gqla_quantize_expanded_fp8_blocks(C.byref(shape), C.byref(expanded), C.byref(expanded_blocks), _stream(stream)),
+           "gqla_quantize_expanded_fp8_blocks")
+
+
+def gqla_decode_gqa_fp8_blocks(shape, plan, q_c, q_r, expanded_blocks: gqla_cache, out, lse, ws, ws_bytes=None, stream=None):
+    nbytes = ws_bytes if ws_bytes is not None else ws.numel() * ws.element_size()
+    _check(lib().gqla_decode_gqa_fp8_blocks(C.byref(shape), plan, _ptr(q_c), _ptr(q_r), C.byref(expanded_blocks), _ptr(out), _ptr(lse),
+                                            _ptr(ws), nbytes, _stream(stream)), "gqla_decode_gqa_fp8_blocks")
+
+
+def gqla_append_expanded(shape, rows: gqla_new_rows, rope_base, expanded: gqla_cache, stream=None):
+    _check(lib().gqla_append_expanded(C.byref(shape), C.byref(rows), float(rope_base), C.byref(expanded), _stream(stream)),
+           "gqla_append_expanded")
+
+
+def gqla_append_expanded_fp8_blocks(shape, rows: gqla_new_rows, rope_base, expanded_blocks: gqla_cache, stream=None):
+    _check(lib().gqla_append_expanded_fp8_blocks(C.byref(shape), C.byref(rows), float(rope_base), C.byref(expanded_blocks),
+                                                 _stream(stream)), "gqla_append_expanded_fp8_blocks")
+
+
+def gqla_attend_gqa_fp8_blocks(shape, first, total, q_c, q_r, expanded_blocks: gqla_cache, out, lse, ws=None, ws_bytes=None, stream=None):
+    if ws_bytes is None:
+        ws_bytes = ws.numel() * ws.element_size() if ws is not None else 0
+    _check(lib().gqla_attend_gqa_fp8_blocks(C.byref(shape), _ptr(first), int(total), _ptr(q_c), _ptr(q_r), C.byref(expanded_blocks),
+                                            _ptr(out), _ptr(lse), _ptr(ws), ws_bytes, _stream(stream)), "gqla_attend_gqa_fp8_blocks")
+
+
+def gqla_attend_gqa_workspace_bytes(shape, first, total, expanded_blocks: gqla_cache) -> int:
+    return lib().gqla_attend_gqa_workspace_bytes(C.byref(shape), _ptr(first), int(total), C.byref(expanded_blocks))
+
+
+def gqla_expanded_fp8_blocks_page_bytes(groups, d_h, d_v, d_r, page_size) -> int:
+    return lib().gqla_expanded_fp8_blocks_page_bytes(groups, d_h, d_v, d_r, page_size)
 
 
 def gqla_expand_cache_tail_fp8(shape, latent: gqla_cache, w_uk, w_uv, group_begin, group_count, expanded_fp8: gqla_cache,

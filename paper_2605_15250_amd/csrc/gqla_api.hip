@@ -822,6 +822,174 @@ gqla_status gqla_decode_gqa_fp8(const gqla_shape* shape, const gqla_plan* plan, 
   return e == hipSuccess ? GQLA_OK : GQLA_ERR_DEVICE;
 }
 
+// ---- the expanded cache with a scale per block of tokens and group -----------------------------------------------------
+gqla_status gqla_quantize_expanded_fp8_blocks(const gqla_shape* shape, const gqla_cache* expanded, const gqla_cache* expanded_blocks,
+                                              void* stream) {
+  gqla_status st = check_shape_expanded(shape);
+  if (st != GQLA_OK) return st;
+  if (shape->dtype != GQLA_BF16) return GQLA_ERR_DTYPE;
+  if (!expanded || !expanded_blocks || !expanded->seq_lens) return GQLA_ERR_NULL;
+  if (expanded->groups <= 0 || expanded->groups > shape->g || expanded->groups != expanded_blocks->groups) return GQLA_ERR_SHAPE;
+  st = check_page_size(shape, expanded->page_size);
+  if (st == GQLA_OK) st = check_cache(shape, expanded, expanded->page_size, 0);
+  if (st == GQLA_OK) st = check_cache(shape, expanded_blocks, expanded->page_size, 0);
+  if (st != GQLA_OK) return st;
+  if (expanded->max_pages != expanded_blocks->max_pages) return GQLA_ERR_PAGE;
+  if (shape->batch == 0) return GQLA_OK;
+  QuantizeArgs a = {};
+  a.src = view_of(expanded);
+  a.dst = view_of(expanded_blocks);
+  a.seq_lens = expanded->seq_lens;
+  a.B = shape->batch;
+  const hipError_t e = launch_quantize_blocks(a, shape->d_h, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? GQLA_OK : GQLA_ERR_DEVICE;
+}
+
+gqla_status gqla_decode_gqa_fp8_blocks(const gqla_shape* shape, const gqla_plan* plan, const void* q_c, const void* q_r,
+                                       const gqla_cache* expanded_blocks, void* out, float* lse, void* ws, size_t ws_bytes,
+                                       void* stream) {
+  gqla_status st = check_shape_expanded(shape);
+  if (st != GQLA_OK) return st;
+  if (shape->dtype != GQLA_BF16) return GQLA_ERR_DTYPE;
+  st = check_decode_common(shape, plan, GQLA_PATH_GQA, expanded_blocks, q_c, q_r, out, lse, ws, ws_bytes);
+  if (st != GQLA_OK) return st;
+  if (expanded_blocks->groups != shape->g) return GQLA_ERR_SHAPE;
+  if (shape->batch == 0) return GQLA_OK;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const DecodeArgs a = decode_args(shape, plan, q_c, q_r, expanded_blocks, ws);
+  CombineArgs c = combine_args(shape, plan, ws, nullptr, out, lse);
+  c.d_h = value_dim(shape);  // partials and outputs are value dims
+  const KernelTimer timer(s);
+  hipError_t e = timer.begin();
+  if (e == hipSuccess) e = launch_decode_gqa_fp8_blocks(a, s);
+  if (e == hipSuccess) e = timer.end();
+  if (e == hipSuccess) e = launch_combine_gqa_bf16(c, s);
+  return e == hipSuccess ? GQLA_OK : GQLA_ERR_DEVICE;
+}
+
+int64_t gqla_expanded_fp8_blocks_page_bytes(int32_t groups, int32_t d_h, int32_t d_v, int32_t d_r, int32_t page_size) {
+  if (groups <= 0 || d_h <= 0 || d_v <= 0 || d_r <= 0 || page_size <= 0 || page_size % 32) return 0;
+  return page_size * (groups * ((int64_t)d_h + d_v) + 2ll * d_r) + (int64_t)groups * (page_size / 32) * 8;
+}
+
+namespace {
+// what packed rows and the expanded cache that they go with have to satisfy
+gqla_status check_packed(const gqla_shape* shape, const int32_t* first, int32_t total, const gqla_cache* expanded) {
+  gqla_status st = check_shape_expanded(shape);
+  if (st != GQLA_OK) return st;
+  if (!expanded || !expanded->pool || !expanded->seq_lens) return GQLA_ERR_NULL;
+  if ((reinterpret_cast<uintptr_t>(first) & 3u) || (reinterpret_cast<uintptr_t>(expanded->seq_lens) & 3u)) return GQLA_ERR_ALIGN;
+  if (total < 0 || total > (1 << 30) || shape->batch > (1 << 24) || expanded->groups != shape->g) return GQLA_ERR_SHAPE;
+  if (!first && total != (int64_t)shape->batch * shape->s_q) return GQLA_ERR_SHAPE;
+  st = check_page_size(shape, expanded->page_size);
+  return st == GQLA_OK ? check_cache(shape, expanded, expanded->page_size, 0) : st;
+}
+
+gqla_status append_impl(const gqla_shape* shape, const gqla_new_rows* rows, float rope_base, const gqla_cache* expanded, void* stream,
+                        bool blocks) {
+  if (!rows) return GQLA_ERR_NULL;
+  gqla_status st = check_packed(shape, rows->first, rows->total, expanded);
+  if (st != GQLA_OK) return st;
+  if (blocks && shape->dtype != GQLA_BF16) return GQLA_ERR_DTYPE;
+  if (!rows->k_c || !rows->v || !rows->k_r || !rows->q_r != !rows->q_rot) return GQLA_ERR_NULL;
+  if (!aligned16(rows->k_c) || !aligned16(rows->v) || !aligned16(rows->k_r) || !aligned16(rows->q_r) || !aligned16(rows->q_rot))
+    return GQLA_ERR_ALIGN;
+  if (!(rope_base == 0.0f || (rope_base > 1.0f && std::isfinite(rope_base))) || shape->d_r % 2 || shape->d_r > 512) return GQLA_ERR_SHAPE;
+  const int64_t d_v = value_dim(shape);
+  auto stride = [&st](int64_t given, int64_t row) -> int64_t {
+    if (given == 0) return row;
+    if (given < row) st = GQLA_ERR_SHAPE;
+    else if (given % 8) st = GQLA_ERR_ALIGN;
+    return given;
+  };
+  AppendRowsArgs a;
+  a.k_stride = stride(rows->k_stride, (int64_t)shape->g * shape->d_h);
+  a.v_stride = stride(rows->v_stride, shape->g * d_v);
+  a.kr_stride = stride(rows->kr_stride, shape->d_r);
+  if (st != GQLA_OK) return st;
+  if (shape->batch == 0 || rows->total == 0) return GQLA_OK;
+  a.k_c = rows->k_c;
+  a.v = rows->v;
+  a.k_r = rows->k_r;
+  a.q_r = rows->q_r;
+  a.q_rot = rows->q_rot;
+  a.first = rows->first;
+  a.seq_lens = expanded->seq_lens;
+  a.cache = view_of(expanded);
+  a.log2_base = rope_base > 0.f ? std::log2((double)rope_base) : 0.0;
+  a.B = shape->batch;
+  a.total = rows->total;
+  a.s_q = shape->s_q;
+  a.h_q = shape->h_q;
+  a.g = shape->g;
+  a.d_h = shape->d_h;
+  a.d_v = (int32_t)d_v;
+  a.d_r = shape->d_r;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const hipError_t e = blocks ? launch_append_rows_fp8_blocks(a, s)
+                              : shape->dtype == GQLA_BF16 ? launch_append_rows_bf16(a, s) : launch_append_rows_f32(a, s);
+  return e == hipSuccess ? GQLA_OK : GQLA_ERR_DEVICE;
+}
+
+int attend_splits_of(const gqla_shape* shape, int32_t total, const gqla_cache* expanded) {
+  return attend_splits(total, shape->batch, shape->h_q, shape->g, shape->d_h, (int64_t)expanded->max_pages * expanded->page_size);
+}
+size_t attend_bytes(const gqla_shape* shape, int32_t total, int splits) {
+  return splits > 1 ? (size_t)splits * total * shape->h_q * (value_dim(shape) + 1) * sizeof(float) : 0;
+}
+}  // namespace
+
+gqla_status gqla_append_expanded(const gqla_shape* shape, const gqla_new_rows* rows, float rope_base, const gqla_cache* expanded,
+                                 void* stream) {
+  return append_impl(shape, rows, rope_base, expanded, stream, false);
+}
+gqla_status gqla_append_expanded_fp8_blocks(const gqla_shape* shape, const gqla_new_rows* rows, float rope_base,
+                                            const gqla_cache* expanded_blocks, void* stream) {
+  return append_impl(shape, rows, rope_base, expanded_blocks, stream, true);
+}
+
+size_t gqla_attend_gqa_workspace_bytes(const gqla_shape* shape, const int32_t* first, int32_t total, const gqla_cache* expanded_blocks) {
+  if (check_packed(shape, first, total, expanded_blocks) != GQLA_OK || shape->dtype != GQLA_BF16 || total == 0 || shape->batch == 0) return 0;
+  return attend_bytes(shape, total, attend_splits_of(shape, total, expanded_blocks));
+}
+
+gqla_status gqla_attend_gqa_fp8_blocks(const gqla_shape* shape, const int32_t* first, int32_t total, const void* q_c, const void* q_r,
+                                       const gqla_cache* expanded_blocks, void* out, float* lse, void* ws, size_t ws_bytes,
+                                       void* stream) {
+  gqla_status st = check_packed(shape, first, total, expanded_blocks);
+  if (st != GQLA_OK) return st;
+  if (shape->dtype != GQLA_BF16) return GQLA_ERR_DTYPE;
+  if (!q_c || !q_r || !out) return GQLA_ERR_NULL;
+  if (!aligned16(q_c) || !aligned16(q_r) || !aligned16(out) || !aligned16(ws) || (reinterpret_cast<uintptr_t>(lse) & 3u)) return GQLA_ERR_ALIGN;
+  if (shape->batch == 0 || total == 0) return GQLA_OK;
+  AttendArgs a;
+  a.G = shape->h_q / shape->g;
+  a.splits = attend_splits_of(shape, total, expanded_blocks);
+  // (row runs, 32 rows each at the least, of all groups and splits are workgroups of one launch)
+  if ((int64_t)total * a.G > INT32_MAX || ((int64_t)total * a.G / 32 + shape->batch) * shape->g > INT32_MAX / a.splits ||
+      (int64_t)total * shape->h_q > INT32_MAX)
+    return GQLA_ERR_SHAPE;
+  if (a.splits > 1 && (!ws || ws_bytes < attend_bytes(shape, total, a.splits))) return GQLA_ERR_WORKSPACE;
+  a.q_c = q_c;
+  a.q_r = q_r;
+  a.out = out;
+  a.lse = lse;
+  a.first = first;
+  a.seq_lens = expanded_blocks->seq_lens;
+  a.cache = view_of(expanded_blocks);
+  a.part_o = static_cast<float*>(ws);
+  a.part_lse = a.splits > 1 ? a.part_o + (size_t)a.splits * total * shape->h_q * value_dim(shape) : nullptr;
+  a.B = shape->batch;
+  a.total = total;
+  a.s_q = shape->s_q;
+  a.h_q = shape->h_q;
+  a.g = shape->g;
+  a.d_h = shape->d_h;
+  a.d_v = value_dim(shape);
+  a.scale_log2e = resolved_scale(shape) * 1.4426950408889634f;
+  return launch_attend_fp8_blocks(a, static_cast<hipStream_t>(stream)) == hipSuccess ? GQLA_OK : GQLA_ERR_DEVICE;
+}
+
 gqla_status gqla_quantize_latent(const gqla_shape* shape, const gqla_cache* latent, const gqla_cache* latent_fp8,
                                  float c_scale, void* stream) {
   gqla_status st = check_shape(shape);

@@ -23,13 +23,13 @@ constexpr float kRescaleThreshold = 8.f;  // log2 units
 // the header's format), widened to bf16 in registers right before their MFMAs; the scales enter once per tile (K: on
 // the content part of the logits, before the RoPE part is added) and once per chunk (V: on the normalised output).
 // Half the bytes per token, the same MFMAs.
-__device__ __forceinline__ bf16x8 widen_e4m3(uint32_t w0, uint32_t w1) {
-  // one instruction per two codes (v_cvt_scalef32_pk_bf16_fp8 with scale 1): exact, every E4M3 value is a bf16 value;
+__device__ __forceinline__ bf16x8 widen_e4m3(uint32_t w0, uint32_t w1, float scale = 1.0f) {
+  // one instruction per two codes (v_cvt_scalef32_pk_bf16_fp8; scale: a power of two): exact, every E4M3 value is a bf16 value;
   // checked on the chip against the fp32 route (v_cvt_pk_f32_fp8, then round to bf16) for all 256 codes in all four
   // byte positions
   typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
-  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, 1.0f, true);
-  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, 1.0f, true);
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, scale, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, scale, true);
   const u32x4 r = {__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, c), __builtin_bit_cast(uint32_t, d)};
   return __builtin_bit_cast(bf16x8, r);
 }
@@ -46,13 +46,18 @@ __device__ __forceinline__ bf16x8 widen_e4m3(uint32_t w0, uint32_t w1) {
 // workgroup share one item, wave w of the team taking tiles w, w + tt, ...; their partial states (m, l, O^T) are merged
 // through LDS, so that one partial per item reaches memory.
 // DEEP (8-bit codes, RB = 1, no teams, shared k_R): the codes of two tiles in registers, see the loop.
-template <int DH, int DV, int DR, bool FP8, int MAXT, int RB, bool TEAM, bool DEEP>
+// BLK (8-bit codes): a power of two per (32 tokens, group) for K and for V instead of k_scale and v_scale.  A tile's pair comes
+// through the scalar cache with the request of its codes and enters where they are widened, at no instruction.  The
+// denominator sums the probabilities ahead of their rounding to bf16 (which saves unpacking them: 2^-9 of each, at random, stays in the
+// output, and the log-sum-exp is as exact as fp32 has it).
+template <int DH, int DV, int DR, bool FP8, int MAXT, int RB, bool TEAM, bool DEEP, bool BLK = false>
 __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int n_items, int row_blocks, int share_kr_arg,
                                                                int tt_arg, float k_scale, float v_scale) {
   constexpr int KS_C = DH / 16;  // k-steps over the content dims
   constexpr int KS_R = DR / 16;  // k-steps over the RoPE dims
   constexpr int MT = DV / 32;    // 32-dim tiles of the output
-  static_assert(!FP8 || DH == DV, "the 8-bit page format is written for equal dims");
+  static_assert(!FP8 || BLK || DH == DV, "the 8-bit page format with one scale is written for equal dims");
+  static_assert(!BLK || FP8, "block scales belong to codes");
   static_assert(!TEAM || RB == 1, "the merge below is written for one row block");
   static_assert(!DEEP || (FP8 && RB == 1 && !TEAM), "two tiles of codes fit the registers of this form only");
   const int tt = TEAM ? tt_arg : 1;
@@ -113,7 +118,7 @@ __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int
   const int P = a.cache.page_size;
   const int gc = a.cache.groups;
   constexpr int EB = FP8 ? 1 : 2;                                             // bytes per K_C / V element
-  const int64_t page_bytes = (int64_t)P * (gc * (DH + DV) * EB + DR * 2);
+  const int64_t page_bytes = (int64_t)P * (gc * (DH + DV) * EB + DR * 2) + (BLK ? (int64_t)gc * (P / 32) * 8 : 0);
   const int64_t kr_plane = (int64_t)gc * (DH + DV) * P * EB;                   // byte offset of the k_R plane in a page
   const char* pool = (const char*)a.cache.pool;
 
@@ -122,6 +127,14 @@ __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int
   u32x4 kf8[DEEP ? 2 : 1][FP8 ? KS_C / 2 : 1], vf8[DEEP ? 2 : 1][FP8 ? MT : 1];
 
   bool k_ok = true, v_ok = true;
+
+  f32x2 blk_scale[DEEP ? 2 : 1];   // BLK: of the tiles whose codes are in registers, for K and V
+  auto load_scales = [&](int tok, int32_t pg) -> f32x2 {
+    typedef const __attribute__((address_space(4))) f32x2* const_ptr_t;
+    const char* at = pool + (int64_t)(pg >= 0 ? pg : 0) * page_bytes + kr_plane + (int64_t)DR * 2 * P + ((int64_t)j * (P / 32) + tok % P / 32) * 8;
+    const f32x2 v = *(const_ptr_t)(uintptr_t)at;
+    return pg >= 0 ? v : f32x2{1.f, 1.f};
+  };
 
   // The shared RoPE key of a tile is the same for every group.  When all waves of a workgroup are groups of one
   // (chunk, row block) -- 8 waves for g a multiple of 8, g waves for g = 2 or 4 -- the tile's k_R (4 KB) is brought
@@ -141,6 +154,7 @@ __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int
   };
   auto load_k = [&](int tok, int32_t pg) {
     k_ok = pg >= 0;
+    if constexpr (BLK) blk_scale[0] = load_scales(tok, pg);
     const char* base = pool + (int64_t)(k_ok ? pg : 0) * page_bytes;
     const int slot = tok % P + n;
     const char* kb = base + (int64_t)j * DH * P * EB + ((int64_t)h * P + slot) * 16;   // vector index h (+ 2 per step below)
@@ -164,7 +178,7 @@ __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int
       const int T = (tok % P) / 32;  // 32-token tile of the page: [T][dim][half] vectors
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt)
-        vf8[0][mt] = __builtin_nontemporal_load((const u32x4*)(base + ((((int64_t)T * DH + mt * 32 + n) * 2 + h) * 16)));
+        vf8[0][mt] = __builtin_nontemporal_load((const u32x4*)(base + ((((int64_t)T * DV + mt * 32 + n) * 2 + h) * 16)));
     } else {
       const int tb = (tok % P) / 8 + h;  // 8-token block of this lane for k-step 0; k-step 1 is two blocks further
 #pragma unroll
@@ -187,7 +201,7 @@ __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int
   };
   auto load_v_codes = [&](u32x4 (&to)[FP8 ? MT : 1], int tok, int32_t pg, bool live) {
     const char* base = pool + (int64_t)(pg >= 0 ? pg : 0) * page_bytes + (int64_t)gc * DH * P + (int64_t)j * DV * P;
-    const uint32_t off = live ? (((tok % P) / 32 * DH + n) * 2 + h) * 16 : 0;   // 32-token tile T of the page: [T][dim][half] vectors
+    const uint32_t off = live ? (((tok % P) / 32 * DV + n) * 2 + h) * 16 : 0;   // 32-token tile T of the page: [T][dim][half] vectors
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) to[mt] = __builtin_nontemporal_load((const u32x4*)(base + mt * 1024 + off));
   };
@@ -228,16 +242,23 @@ __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int
     auto tile = [&](int tok, auto which, int slot, bool active) __attribute__((always_inline)) {
       constexpr int W = decltype(which)::value;
       f32x16 s;
+      float sc_k = 1.f, sc_v = 1.f;
+      if constexpr (BLK) {
+        sc_k = blk_scale[W][0];
+        sc_v = blk_scale[W][1];
+      }
       if (active) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
         for (int ks = 0; ks < KS_C; ++ks) {
           const u32x4 c = kf8[W][ks / 2];
-          s = mfma32((ks & 1) ? widen_e4m3(c[2], c[3]) : widen_e4m3(c[0], c[1]), qc[0][ks], s);
+          s = mfma32((ks & 1) ? widen_e4m3(c[2], c[3], sc_k) : widen_e4m3(c[0], c[1], sc_k), qc[0][ks], s);
         }
+        if constexpr (!BLK) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] *= k_scale;
+          for (int i = 0; i < 16; ++i) s[i] *= k_scale;
+        }
         // behind this tile's k_R (loads complete in issue order): its key and value codes and the next tile's
         static_assert(KS_C + 2 * MT == 16, "the wait below is written for this count");
         asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
@@ -257,6 +278,9 @@ __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int
       }
       codes_ok[W] = pg_next >= 0;
       if (live) stage_kr(ahead, pg_next, slot == 0 ? 2 : slot - 1);   // (slot + 2) mod 3: read ahead of this tile's barrier
+      if constexpr (BLK) {
+        if (live) blk_scale[W] = load_scales(ahead, pg_next);
+      }
       load_k_codes(kf8[W], ahead, pg_next, live);
       if (ahead + tstep < ce.tok_end) lookup_start(ahead + tstep, pg_raw);
 
@@ -293,8 +317,13 @@ __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int
         for (int kk = 0; kk < 2; ++kk) {
           const uint32_t x0 = pack_bf16(sv[8 * kk + 0], sv[8 * kk + 1]), x1 = pack_bf16(sv[8 * kk + 2], sv[8 * kk + 3]);
           const uint32_t y0 = pack_bf16(sv[8 * kk + 4], sv[8 * kk + 5]), y1 = pack_bf16(sv[8 * kk + 6], sv[8 * kk + 7]);
+          if constexpr (BLK) {
 #pragma unroll
-          for (uint32_t wd : {x0, x1, y0, y1}) psum += __builtin_bit_cast(float, wd << 16) + __builtin_bit_cast(float, wd & 0xffff0000u);
+            for (int i = 0; i < 8; ++i) psum += sv[8 * kk + i];
+          } else {
+#pragma unroll
+            for (uint32_t wd : {x0, x1, y0, y1}) psum += __builtin_bit_cast(float, wd << 16) + __builtin_bit_cast(float, wd & 0xffff0000u);
+          }
           u32x4 w;
           uint32_t r0, r1;
           half_swap(x0, y0, r0, r1);
@@ -318,7 +347,7 @@ __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-          for (int kk = 0; kk < 2; ++kk) o[0][mt] = mfma32(widen_e4m3(vf8[W][mt][2 * kk], vf8[W][mt][2 * kk + 1]), pf[kk], o[0][mt]);
+          for (int kk = 0; kk < 2; ++kk) o[0][mt] = mfma32(widen_e4m3(vf8[W][mt][2 * kk], vf8[W][mt][2 * kk + 1], sc_v), pf[kk], o[0][mt]);
       }
       asm volatile("" ::: "memory");
       load_v_codes(vf8[W], ahead, pg_next, live);
@@ -331,6 +360,7 @@ __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int
       pg_next = checked(pg_raw);
       codes_ok[0] = pg_next >= 0;
       stage_kr(tok0, pg_next, 0);
+      if constexpr (BLK) blk_scale[0] = blk_scale[1] = load_scales(tok0, pg_next);
       load_k_codes(kf8[0], tok0, pg_next, true);
       asm volatile("" ::: "memory");   // (keys first: the tile's products begin with them)
       load_v_codes(vf8[0], tok0, pg_next, true);
@@ -343,6 +373,9 @@ __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int
       }
       codes_ok[1] = pg_next >= 0;
       if (live) stage_kr(tok1, pg_next, 1);
+      if constexpr (BLK) {
+        if (live) blk_scale[1] = load_scales(tok1, pg_next);
+      }
       load_k_codes(kf8[1], tok1, pg_next, live);
       asm volatile("" ::: "memory");
       load_v_codes(vf8[1], tok1, pg_next, live);
@@ -373,17 +406,22 @@ __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[x][i] = 0.f;
       if constexpr (FP8) {
+        float sc_k = 1.f, sc_v = 1.f;
+        if constexpr (BLK) {
+          sc_k = blk_scale[0][0];
+          sc_v = blk_scale[0][1];
+        }
 #pragma unroll
         for (int kp = 0; kp < KS_C / 2; ++kp) {
-          kf[2 * kp] = widen_e4m3(kf8[0][kp][0], kf8[0][kp][1]);
-          kf[2 * kp + 1] = widen_e4m3(kf8[0][kp][2], kf8[0][kp][3]);
+          kf[2 * kp] = widen_e4m3(kf8[0][kp][0], kf8[0][kp][1], sc_k);
+          kf[2 * kp + 1] = widen_e4m3(kf8[0][kp][2], kf8[0][kp][3], sc_k);
         }
         // the value codes are widened here as well: their registers are then free for the next tile's codes, which are
         // requested together with the key codes (twice the bytes in flight per wave)
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
-          vf[mt][0] = widen_e4m3(vf8[0][mt][0], vf8[0][mt][1]);
-          vf[mt][1] = widen_e4m3(vf8[0][mt][2], vf8[0][mt][3]);
+          vf[mt][0] = widen_e4m3(vf8[0][mt][0], vf8[0][mt][1], sc_v);
+          vf[mt][1] = widen_e4m3(vf8[0][mt][2], vf8[0][mt][3], sc_v);
         }
       }
       const bool tile_v_ok = v_ok;  // v_ok is overwritten by the next tile's request below (FP8)
@@ -392,7 +430,7 @@ __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int
       for (int ks = 0; ks < KS_C; ++ks)
 #pragma unroll
         for (int x = 0; x < RB; ++x) s[x] = mfma32(kf[ks], q_content(x, ks), s[x]);
-      if constexpr (FP8) {
+      if constexpr (FP8 && !BLK) {
 #pragma unroll
         for (int x = 0; x < RB; ++x)
 #pragma unroll
@@ -402,8 +440,9 @@ __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int
         // this tile's k_R was requested before the cache loads that followed it (loads complete in issue order): the
         // tile's key and value vectors, 16-byte loads each -- KS_C + 2*MT of them in 16 bits, half as many as codes
         constexpr int kLoadsBehindKr = FP8 ? KS_C / 2 + MT : KS_C + 2 * MT;
-        static_assert(kLoadsBehindKr == 8 || kLoadsBehindKr == 16 || kLoadsBehindKr == 28, "the wait below is written for these counts");
+        static_assert(kLoadsBehindKr == 8 || kLoadsBehindKr == 14 || kLoadsBehindKr == 16 || kLoadsBehindKr == 28, "the wait below is written for these counts");
         if constexpr (kLoadsBehindKr == 8) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+        else if constexpr (kLoadsBehindKr == 14) asm volatile("s_waitcnt vmcnt(14)" ::: "memory");
         else if constexpr (kLoadsBehindKr == 16) asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
         else asm volatile("s_waitcnt vmcnt(28)" ::: "memory");
         __syncthreads();
@@ -471,8 +510,13 @@ __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int
         for (int kk = 0; kk < 2; ++kk) {
           const uint32_t x0 = pack_bf16(sv[8 * kk + 0], sv[8 * kk + 1]), x1 = pack_bf16(sv[8 * kk + 2], sv[8 * kk + 3]);
           const uint32_t y0 = pack_bf16(sv[8 * kk + 4], sv[8 * kk + 5]), y1 = pack_bf16(sv[8 * kk + 6], sv[8 * kk + 7]);
+          if constexpr (BLK) {
 #pragma unroll
-          for (uint32_t wd : {x0, x1, y0, y1}) psum += __builtin_bit_cast(float, wd << 16) + __builtin_bit_cast(float, wd & 0xffff0000u);
+            for (int i = 0; i < 8; ++i) psum += sv[8 * kk + i];
+          } else {
+#pragma unroll
+            for (uint32_t wd : {x0, x1, y0, y1}) psum += __builtin_bit_cast(float, wd << 16) + __builtin_bit_cast(float, wd & 0xffff0000u);
+          }
           u32x4 w;
           uint32_t r0, r1;
           half_swap(x0, y0, r0, r1);
@@ -541,7 +585,7 @@ __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int
       }
     }
     const bool ok = row_ok[0];
-    const float inv = (l_all > 0.f ? 1.f / l_all : 0.f) * (FP8 ? v_scale : 1.f);
+    const float inv = (l_all > 0.f ? 1.f / l_all : 0.f) * (FP8 && !BLK ? v_scale : 1.f);
     const int rho = t_of[0] * a.h_q + head_of[0];
     const int64_t prow = (int64_t)chunk * a.M + rho;
     // chunk partial in fp32, 4-dim vectors ordered [chunk][32-row block][d_v / 4][row] (part_vec_index): this lane
@@ -570,7 +614,7 @@ __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int
   for (int x = 0; x < RB; ++x) {
     const float l_tot = pair_sum(l_run[x]);
     if (!row_ok[x]) continue;
-    const float inv = (l_tot > 0.f ? 1.f / l_tot : 0.f) * (FP8 ? v_scale : 1.f);
+    const float inv = (l_tot > 0.f ? 1.f / l_tot : 0.f) * (FP8 && !BLK ? v_scale : 1.f);
     const int rho = t_of[x] * a.h_q + head_of[x];
     const int64_t prow = (int64_t)chunk * a.M + rho;
     // chunk partial in fp32, 4-dim vectors ordered [chunk][32-row block][d_v / 4][row] (part_vec_index): consecutive rows
@@ -753,17 +797,17 @@ constexpr int gqa_merge_bytes(int waves) { return waves * (DV / 32 * 4 * 64 * 16
 // two or four groups (64 ragged sequences of 3000 to 12000 tokens, 4 groups 101 us against 106), k_R not shared (32 x 4096, 3 groups
 // 29.7 against 32.8), two row blocks a wave (64 ragged, 48 rows of 8 groups 340 against 364).
 static bool gqa_codes_deep(const DecodeArgs& a) { return a.g % 8 == 0 && a.chunk_tiles >= 4 && 2 * a.chunk_tiles > a.G * a.s_q; }
-template <bool FP8>
+template <bool FP8, bool BLK = false>
 static hipError_t launch_decode_gqa_128(const DecodeArgs& a, float k_scale, float v_scale, hipStream_t s) {
   int row_blocks, n_items, wpb, blocks;
   bool team;
   if (a.G * a.s_q > 32) {  // more than one row block per group: two per wave, four waves per workgroup
     gqa_launch_shape(a, 4, 64, row_blocks, n_items, team, wpb, blocks);
     constexpr int kQBytesPerWave = 2 * (128 / 16 + 64 / 16) * 1024;  // both row blocks' query fragments
-    static const hipError_t attr = hipFuncSetAttribute((const void*)decode_gqa_bf16_kernel<128, 128, 64, FP8, 256, 2, false, false>,
+    static const hipError_t attr = hipFuncSetAttribute((const void*)decode_gqa_bf16_kernel<128, 128, 64, FP8, 256, 2, false, false, BLK>,
                                                        hipFuncAttributeMaxDynamicSharedMemorySize, 4 * kQBytesPerWave);
     if (attr != hipSuccess) return attr;
-    decode_gqa_bf16_kernel<128, 128, 64, FP8, 256, 2, false, false><<<blocks, 64 * wpb, wpb * kQBytesPerWave, s>>>(a, n_items, row_blocks, team ? 1 : 0,
+    decode_gqa_bf16_kernel<128, 128, 64, FP8, 256, 2, false, false, BLK><<<blocks, 64 * wpb, wpb * kQBytesPerWave, s>>>(a, n_items, row_blocks, team ? 1 : 0,
                                                                                                     1, k_scale, v_scale);
     return hipGetLastError();
   }
@@ -771,46 +815,53 @@ static hipError_t launch_decode_gqa_128(const DecodeArgs& a, float k_scale, floa
   // one group: the plan cuts chunks for teams of eight
   const int tt = a.g == 1 ? 8 : gqa_token_team_size(a, n_items, 8);
   if (tt > 1) {
-    static const hipError_t attr = hipFuncSetAttribute((const void*)decode_gqa_bf16_kernel<128, 128, 64, FP8, 512, 1, true, false>,
+    static const hipError_t attr = hipFuncSetAttribute((const void*)decode_gqa_bf16_kernel<128, 128, 64, FP8, 512, 1, true, false, BLK>,
                                                        hipFuncAttributeMaxDynamicSharedMemorySize, gqa_merge_bytes<128>(8));
     if (attr != hipSuccess) return attr;
     const int w = gqa_team_waves(a, n_items, tt, 8);
-    decode_gqa_bf16_kernel<128, 128, 64, FP8, 512, 1, true, false><<<(n_items * tt + w - 1) / w, 64 * w, gqa_merge_bytes<128>(w), s>>>(a, n_items, row_blocks, 0, tt,
+    decode_gqa_bf16_kernel<128, 128, 64, FP8, 512, 1, true, false, BLK><<<(n_items * tt + w - 1) / w, 64 * w, gqa_merge_bytes<128>(w), s>>>(a, n_items, row_blocks, 0, tt,
                                                                                                                          k_scale, v_scale);
     return hipGetLastError();
   }
   if constexpr (FP8) {
     if (gqa_codes_deep(a)) {
-      decode_gqa_bf16_kernel<128, 128, 64, true, 512, 1, false, true><<<blocks, 64 * wpb, 0, s>>>(a, n_items, row_blocks, 1, 1, k_scale, v_scale);
+      decode_gqa_bf16_kernel<128, 128, 64, true, 512, 1, false, true, BLK><<<blocks, 64 * wpb, 0, s>>>(a, n_items, row_blocks, 1, 1, k_scale, v_scale);
       return hipGetLastError();
     }
   }
-  decode_gqa_bf16_kernel<128, 128, 64, FP8, 512, 1, false, false><<<blocks, 64 * wpb, 0, s>>>(a, n_items, row_blocks, team ? 1 : 0, 1, k_scale, v_scale);
+  decode_gqa_bf16_kernel<128, 128, 64, FP8, 512, 1, false, false, BLK><<<blocks, 64 * wpb, 0, s>>>(a, n_items, row_blocks, team ? 1 : 0, 1, k_scale, v_scale);
+  return hipGetLastError();
+}
+
+// (d_h, d_v) = (192, 256): four waves per workgroup, one row block each
+template <bool BLK>
+static hipError_t launch_decode_gqa_192(const DecodeArgs& a, hipStream_t s) {
+  int row_blocks, n_items, wpb, blocks;
+  bool team;
+  gqa_launch_shape(a, 4, 32, row_blocks, n_items, team, wpb, blocks);
+  const int tt = gqa_token_team_size(a, n_items, 4);
+  if (tt > 1) {
+    static const hipError_t attr = hipFuncSetAttribute((const void*)decode_gqa_bf16_kernel<192, 256, 64, BLK, 256, 1, true, false, BLK>,
+                                                       hipFuncAttributeMaxDynamicSharedMemorySize, gqa_merge_bytes<256>(4));
+    if (attr != hipSuccess) return attr;
+    const int w = gqa_team_waves(a, n_items, tt, 4);
+    decode_gqa_bf16_kernel<192, 256, 64, BLK, 256, 1, true, false, BLK><<<(n_items * tt + w - 1) / w, 64 * w, gqa_merge_bytes<256>(w), s>>>(a, n_items, row_blocks, 0, tt, 1.f, 1.f);
+    return hipGetLastError();
+  }
+  decode_gqa_bf16_kernel<192, 256, 64, BLK, 256, 1, false, false, BLK><<<blocks, 64 * wpb, 0, s>>>(a, n_items, row_blocks, team ? 1 : 0, 1, 1.f, 1.f);
   return hipGetLastError();
 }
 
 hipError_t launch_decode_gqa_bf16(const DecodeArgs& a, hipStream_t s) {
-  if (a.d_h == 192) {  // (d_h, d_v) = (192, 256): four waves per workgroup, one row block each
-    int row_blocks, n_items, wpb, blocks;
-    bool team;
-    gqa_launch_shape(a, 4, 32, row_blocks, n_items, team, wpb, blocks);
-    const int tt = gqa_token_team_size(a, n_items, 4);
-    if (tt > 1) {
-      static const hipError_t attr = hipFuncSetAttribute((const void*)decode_gqa_bf16_kernel<192, 256, 64, false, 256, 1, true, false>,
-                                                         hipFuncAttributeMaxDynamicSharedMemorySize, gqa_merge_bytes<256>(4));
-      if (attr != hipSuccess) return attr;
-      const int w = gqa_team_waves(a, n_items, tt, 4);
-      decode_gqa_bf16_kernel<192, 256, 64, false, 256, 1, true, false><<<(n_items * tt + w - 1) / w, 64 * w, gqa_merge_bytes<256>(w), s>>>(a, n_items, row_blocks, 0, tt, 1.f, 1.f);
-      return hipGetLastError();
-    }
-    decode_gqa_bf16_kernel<192, 256, 64, false, 256, 1, false, false><<<blocks, 64 * wpb, 0, s>>>(a, n_items, row_blocks, team ? 1 : 0, 1, 1.f, 1.f);
-    return hipGetLastError();
-  }
-  return launch_decode_gqa_128<false>(a, 1.f, 1.f, s);
+  return a.d_h == 192 ? launch_decode_gqa_192<false>(a, s) : launch_decode_gqa_128<false>(a, 1.f, 1.f, s);
 }
 
 hipError_t launch_decode_gqa_fp8(const DecodeArgs& a, float k_scale, float v_scale, hipStream_t s) {
   return launch_decode_gqa_128<true>(a, k_scale, v_scale, s);
+}
+
+hipError_t launch_decode_gqa_fp8_blocks(const DecodeArgs& a, hipStream_t s) {
+  return a.d_h == 192 ? launch_decode_gqa_192<true>(a, s) : launch_decode_gqa_128<true, true>(a, 1.f, 1.f, s);
 }
 
 template <int DV>

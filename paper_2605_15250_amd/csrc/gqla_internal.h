@@ -87,6 +87,30 @@ struct AppendArgs {
   int32_t B, s_q, row_bytes;
 };
 
+struct AppendRowsArgs {
+  const void *k_c, *v, *k_r, *q_r;  // packed rows; q_r, q_rot: both or neither
+  void* q_rot;
+  const int32_t* first;             // int32[B + 1], or null: s_q rows per sequence
+  const int32_t* seq_lens;
+  CacheView cache;                  // expanded: 16-bit, fp32, or 8-bit with block scales
+  int64_t k_stride, v_stride, kr_stride;  // elements from row to row
+  double log2_base;                 // 0: nothing is rotated
+  int32_t B, total, s_q, h_q, g, d_h, d_v, d_r;
+};
+
+struct AttendArgs {
+  const void *q_c, *q_r;            // packed rows [total][h_q][..]
+  void* out;
+  float* lse;                       // optional
+  const int32_t* first;             // as above
+  const int32_t* seq_lens;
+  CacheView cache;                  // 8-bit with block scales
+  float* part_o;                    // splits > 1: [splits][total][h_q][d_v], then the log-sum-exps [splits][total][h_q]
+  float* part_lse;
+  int32_t B, total, s_q, h_q, g, G, d_h, d_v, splits;
+  float scale_log2e;
+};
+
 struct RopeArgs {
   void* q_r;   // [B][s_q][h_q][d_r] or null
   void* rows;  // [B][s_q][row_elems], k_R at column r_kv; or null
@@ -146,6 +170,14 @@ hipError_t launch_out_proj_bf16(const OutProjArgs&, hipStream_t);
 int out_proj_rows(int M, int K, int D);
 int out_proj_split(int M, int K, int D, int rows, int* krange);  // k-ranges of the bf16 kernel (needs D % 128 == 0, K % 256 == 0)
 hipError_t launch_decode_gqa_fp8(const DecodeArgs&, float k_scale, float v_scale, hipStream_t);
+
+hipError_t launch_decode_gqa_fp8_blocks(const DecodeArgs&, hipStream_t);
+hipError_t launch_append_rows_f32(const AppendRowsArgs&, hipStream_t);
+hipError_t launch_append_rows_bf16(const AppendRowsArgs&, hipStream_t);
+hipError_t launch_append_rows_fp8_blocks(const AppendRowsArgs&, hipStream_t);
+hipError_t launch_quantize_blocks(const QuantizeArgs&, int d_h, hipStream_t);  // src: 16-bit expanded cache, dst: block scales
+int attend_splits(int64_t total, int64_t batch, int h_q, int g, int d_h, int64_t max_tokens);
+hipError_t launch_attend_fp8_blocks(const AttendArgs&, hipStream_t);
 
 hipError_t launch_probe_stream_read(const void* src, size_t bytes, uint32_t* sink, int blocks, hipStream_t);
 hipError_t launch_probe_mfma(uint32_t* sink, int iters, int blocks, hipStream_t);

@@ -72,8 +72,10 @@ class Decoder:
         self.expanded_pool = None
         self.expanded_fp8_pool = None
         self.latent_fp8_pool = None
+        self.expanded_blocks_pool = None
         self.ws_e = None                                        # scratch of the expand call
         self.ws_o = None                                        # scratch of the output projection
+        self.ws_t = None                                        # scratch of the prompt chunks' attention
 
     def close(self):
         for p in (self.plan_a, self.plan_g):
@@ -212,6 +214,57 @@ class Decoder:
         if lse is None:
             lse = torch.empty((c.B, c.s_q, heads), dtype=torch.float32, device="cuda")
         B.gqla_decode_gqa_fp8(self.shape_gqa, self.plan_g, q_c, q_r, self.expanded_fp8_cache(), k_scale, v_scale, out, lse, self.ws_g)
+        return out, lse
+
+    # -- rows of new tokens into the expanded caches; 8-bit expanded cache with a scale per block of tokens and group -------
+    def alloc_expanded_blocks(self, fill=0xAA):
+        c = self.cfg
+        nbytes = B.gqla_expanded_fp8_blocks_page_bytes(self.groups, c.d_h, c.dv, c.d_r, c.page_size)
+        self.expanded_blocks_pool = torch.full((self.num_pages * nbytes,), fill, dtype=torch.uint8, device="cuda")
+        return self.expanded_blocks_pool
+
+    def expanded_blocks_cache(self):
+        return B.make_cache(self.expanded_blocks_pool, self.d_lens, self.d_table, self.cfg.page_size, self.max_pages,
+                            self.num_pages, self.groups)
+
+    def quantize_expanded_blocks(self):
+        B.gqla_quantize_expanded_fp8_blocks(self.shape, self.expanded_cache(), self.expanded_blocks_cache())
+        return self.expanded_blocks_pool
+
+    def append_expanded(self, rope_base, k_c, v, k_r, q_r=None, first=None, blocks=False):
+        """New rows k_c [n, groups * d_h], v [n, groups * d_v], k_r [n, d_r] (unit stride inside a row) into the expanded cache, or into the
+        one with block scales; returns the rotated queries.  first: device int32 [B + 1], None: s_q rows per sequence."""
+        q_rot = torch.empty_like(q_r) if q_r is not None else None
+        rows = B.make_new_rows(k_c, v, k_r, q_r, q_rot, first, k_c.shape[0], k_c.stride(0), v.stride(0), k_r.stride(0))
+        if blocks:
+            B.gqla_append_expanded_fp8_blocks(self.shape_gqa, rows, rope_base, self.expanded_blocks_cache())
+        else:
+            B.gqla_append_expanded(self.shape_gqa, rows, rope_base, self.expanded_cache())
+        return q_rot
+
+    def decode_gqa_blocks(self, q_c, q_r, out=None, lse=None):
+        """q_c, q_r: [B, s_q, heads of the slice, d] contiguous."""
+        c = self.cfg
+        if out is None:
+            out = torch.empty(q_c.shape[:3] + (c.dv,), dtype=torch_dtype(c.dtype), device="cuda")
+        if lse is None:
+            lse = torch.empty(q_c.shape[:3], dtype=torch.float32, device="cuda")
+        B.gqla_decode_gqa_fp8_blocks(self.shape_gqa, self.plan_g, q_c, q_r, self.expanded_blocks_cache(), out, lse, self.ws_g)
+        return out, lse
+
+    def attend_gqa_blocks(self, q_c, q_r, first=None, out=None, lse=None):
+        """q_c [n, heads of the slice, d_h], q_r [n, heads, d_r] contiguous: prompt chunks, packed."""
+        c = self.cfg
+        n, heads = q_c.shape[0], q_c.shape[1]
+        if out is None:
+            out = torch.empty((n, heads, c.dv), dtype=torch_dtype(c.dtype), device="cuda")
+        if lse is None:
+            lse = torch.empty((n, heads), dtype=torch.float32, device="cuda")
+        cache = self.expanded_blocks_cache()
+        nbytes = B.gqla_attend_gqa_workspace_bytes(self.shape_gqa, first, n, cache)
+        if nbytes and (self.ws_t is None or self.ws_t.numel() < nbytes):
+            self.ws_t = torch.empty((nbytes,), dtype=torch.uint8, device="cuda")
+        B.gqla_attend_gqa_fp8_blocks(self.shape_gqa, first, n, q_c, q_r, cache, out, lse, self.ws_t if nbytes else None)
         return out, lse
 
     # -- 8-bit latent cache --------------------------------------------------------------------------------
