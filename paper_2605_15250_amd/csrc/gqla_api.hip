@@ -965,6 +965,9 @@ gqla_status gqla_attend_gqa_fp8_blocks(const gqla_shape* shape, const int32_t* f
   AttendArgs a;
   a.G = shape->h_q / shape->g;
   a.splits = attend_splits_of(shape, total, expanded_blocks);
+  // offsets inside a page are 32-bit
+  if (gqla_expanded_fp8_blocks_page_bytes(shape->g, shape->d_h, value_dim(shape), shape->d_r, expanded_blocks->page_size) > INT32_MAX)
+    return GQLA_ERR_SHAPE;
   // (row runs, 32 rows each at the least, of all groups and splits are workgroups of one launch)
   if ((int64_t)total * a.G > INT32_MAX || ((int64_t)total * a.G / 32 + shape->batch) * shape->g > INT32_MAX / a.splits ||
       (int64_t)total * shape->h_q > INT32_MAX)

@@ -118,40 +118,58 @@ __global__ void __launch_bounds__(64 * kWaves, DV == 128 ? 2 : 1) attend_kernel(
     }
   }
 
-  const int64_t page_bytes = (int64_t)P * (gc * (DH + DV) + DR * 2) + (int64_t)gc * (P / 32) * 8;
-  const char* const pool = (const char*)a.cache.pool;
-  auto page_at = [&](int st) { return page_of_uniform(a.cache, r.b, (int)((int64_t)st * kStage / P)); };
-  // requests stage st (this wave's share) into buffer buf
-  const uint32_t off_kr = (h * P + n) * 16, off_v = (n * 2 + h) * 16;
-  auto request = [&](int st, int32_t pg, int buf) __attribute__((always_inline)) {
-    const char* page = pool + (int64_t)(pg >= 0 ? pg : 0) * page_bytes;
-    const int slot0 = (int)((int64_t)st * kStage % P);
-    const uint32_t lds = (uint32_t)(uintptr_t)(lds_ptr_t)(smem + buf * (PIECES * 1024));
 #pragma unroll
-    for (int i = 0; i < Tile::kPer; ++i) {
-      const int piece = wave + kWaves * i;                             // [kind][32-token tile][fragment]
-      const char* src;
-      uint32_t off;
-      if (kWaves * i < 2 * KC) {
-        const int tt = piece / KC, kp = piece % KC;
-        src = page + ((int64_t)(j * (DH / 16) + 2 * kp) * P + slot0 + 32 * tt) * 16;
-        off = off_kr;
-      } else if (kWaves * i < 2 * (KC + KR)) {
-        const int p = piece - 2 * KC, tt = p / KR, ks = p % KR;
-        src = page + (int64_t)P * gc * (DH + DV) + ((int64_t)2 * ks * P + slot0 + 32 * tt) * 16;
-        off = off_kr;
-      } else {
-        const int p = piece - 2 * (KC + KR), tt = p / MT, mt = p % MT;
-        src = page + (int64_t)P * gc * DH + ((int64_t)(j * (P / 32) + slot0 / 32 + tt) * DV + 32 * mt) * 32;
-        off = off_v;
-      }
-      const uint32_t dst = __builtin_amdgcn_readfirstlane(lds + piece * 1024);
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(dst), "v"(off), "s"(src) : "memory");
+  for (int ks = 0; ks < KR; ++ks) asm volatile("" : "+v"(qr[ks]));      // (waited for here: a wait inside the loop would be one for the requests, too)
+
+  // Where this wave's pieces of a stage begin in a page (32 bits: the host has seen to that), for its first slots; a stage further on
+  // in the page adds 64 vectors of 16 bytes to those of K and k_R, 64 * DV bytes to those of V.
+  uint32_t off[Tile::kPer];
+#pragma unroll
+  for (int i = 0; i < Tile::kPer; ++i) {
+    const int piece = wave + kWaves * i;                               // [kind][32-token tile][fragment]
+    if (kWaves * i < 2 * KC) {
+      const int tt = piece / KC, kp = piece % KC;
+      off[i] = ((j * (DH / 16) + 2 * kp + h) * P + 32 * tt + n) * 16;
+    } else if (kWaves * i < 2 * (KC + KR)) {
+      const int p = piece - 2 * KC, tt = p / KR, ks = p % KR;
+      off[i] = P * gc * (DH + DV) + ((2 * ks + h) * P + 32 * tt + n) * 16;
+    } else {
+      const int p = piece - 2 * (KC + KR), tt = p / MT, mt = p % MT;
+      off[i] = P * gc * DH + (((j * (P / 32) + tt) * DV + 32 * mt + n) * 2 + h) * 16;
     }
+  }
+  const uint32_t page_bytes = P * (gc * (DH + DV) + DR * 2) + gc * (P / 32) * 8;
+  const uint32_t scale_off = P * (gc * (DH + DV) + DR * 2) + j * (P / 32) * 8;
+  const char* const pool = (const char*)a.cache.pool;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)smem + wave * 1024;
+  // A stage: its page (-1: not there) and first slot.  Looked up in order, a stage ahead of the requests.
+  struct Stage {
+    int32_t page, slot;
   };
-  auto scales_at = [&](int st, int32_t pg) -> f32x4 {                  // K, V of the stage's first tile, K, V of its second
-    const char* page = pool + (int64_t)(pg >= 0 ? pg : 0) * page_bytes;
-    return *(const_f32x4_ptr)(uintptr_t)(page + (int64_t)P * (gc * (DH + DV) + 2 * DR) + (j * (P / 32) + (int)((int64_t)st * kStage % P) / 32) * 8);
+  int next_page = st0 * kStage / P, next_slot = st0 * kStage % P;
+  auto look_up = [&]() -> Stage {
+    const Stage g = {page_of_uniform(a.cache, r.b, next_page), next_slot};
+    next_slot += kStage;
+    if (next_slot == P) {
+      next_slot = 0;
+      ++next_page;
+    }
+    return g;
+  };
+  auto page_of_stage = [&](Stage g) { return pool + (int64_t)max(g.page, 0) * page_bytes; };   // (one that is not there: any)
+  auto request = [&](Stage g, int buf) __attribute__((always_inline)) {
+    const char* page = page_of_stage(g);
+    const char *kr = page + g.slot * 16, *v = page + g.slot * DV;
+    const uint32_t lds = lds0 + buf * (PIECES * 1024);
+#pragma unroll
+    for (int i = 0; i < Tile::kPer; ++i)
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                   :
+                   : "s"(lds + kWaves * i * 1024), "v"(off[i]), "s"(kWaves * i < 2 * (KC + KR) ? kr : v)
+                   : "memory");
+  };
+  auto scales_of = [&](Stage g) -> f32x4 {                              // K, V of the stage's first tile, K, V of its second
+    return *(const_f32x4_ptr)(uintptr_t)(page_of_stage(g) + scale_off + g.slot / 32 * 8);
   };
 
   f32x16 o[MT];
@@ -233,13 +251,16 @@ __global__ void __launch_bounds__(64 * kWaves, DV == 128 ? 2 : 1) attend_kernel(
   };
 
   if (st0 < st1) {
-    int32_t pg[NB];                                                    // pages of the stages ahead: pg[0] this one's
+    Stage g[NB];                                                       // this stage and those ahead
 #pragma unroll
-    for (int i = 0; i < NB; ++i) pg[i] = st0 + i < st1 ? page_at(st0 + i) : -1;
+    for (int i = 0; i < NB; ++i) {
+      g[i] = Stage{-1, 0};
+      if (st0 + i < st1) g[i] = look_up();
+    }
 #pragma unroll
     for (int i = 0; i < NB - 1; ++i)
-      if (st0 + i < st1) request(st0 + i, pg[i], i);
-    f32x4 sc = scales_at(st0, pg[0]);
+      if (st0 + i < st1) request(g[i], i);
+    f32x4 sc = scales_of(g[0]);
     int buf = 0;
     for (int st = st0; st < st1; ++st) {
       // this stage's requests are the oldest: those of the NB - 2 stages behind it may be on their way still
@@ -250,16 +271,15 @@ __global__ void __launch_bounds__(64 * kWaves, DV == 128 ? 2 : 1) attend_kernel(
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       }
       __syncthreads();                                                 // every wave's share is there; the buffer before is free
-      const int ahead = st + NB - 1;
-      if (ahead < st1) request(ahead, pg[NB - 1], buf == 0 ? NB - 1 : buf - 1);
-      const int32_t here = pg[0];
+      if (st + NB - 1 < st1) request(g[NB - 1], buf == 0 ? NB - 1 : buf - 1);
+      const bool there = g[0].page >= 0;
 #pragma unroll
-      for (int i = 0; i + 1 < NB; ++i) pg[i] = pg[i + 1];
+      for (int i = 0; i + 1 < NB; ++i) g[i] = g[i + 1];
       const f32x4 now = sc;
-      if (st + 1 < st1) sc = scales_at(st + 1, pg[0]);
-      if (ahead + 1 < st1) pg[NB - 1] = page_at(ahead + 1);
+      if (st + 1 < st1) sc = scales_of(g[0]);
+      if (st + NB < st1) g[NB - 1] = look_up();
       const int tok = st * kStage;
-      if (here >= 0) {                                                 // a page that is not there holds nothing
+      if (there) {                                                     // a page that is not there holds nothing
         const char* lds = smem + buf * (PIECES * 1024) + lane * 16;
         if (tok < vis_max) attend_tile(tok, lds, lds + 2 * KC * 1024, lds + 2 * (KC + KR) * 1024, now[0], now[1]);
         if (tok + 32 < vis_max)
