@@ -39,16 +39,17 @@ template <int DH, int DV>
 struct AttendTile {
   static constexpr int KC = DH / 32, KR = 4, MT = DV / 32;             // 1 KB pieces per 32 tokens: K codes, k_R, V codes
   static constexpr int kPieces = 2 * (KC + KR + MT), kPer = kPieces / kWaves;
-  static constexpr int kBuffers = DV == 128 ? 3 : 2;
   static constexpr int kPitch = DV * 2 + 16;                           // of an output row on its way through LDS
-  static constexpr int kLds = std::max(kBuffers * kPieces * 1024, kRows * kPitch);
+  static constexpr int kState = MT * 4096 + 512;                       // a wave's O^T, maxima and sums on their way to another wave
+  static constexpr int kPerUnit = DV == 128 ? 3 : 2;                   // workgroups of a compute unit (registers; three rings of 48 KB)
+  static constexpr int kLds = std::max(2 * kPieces * 1024, std::max(kRows * kPitch, 2 * kState));
   static_assert(2 * KC % kWaves == 0 && 2 * KR % kWaves == 0 && 2 * MT % kWaves == 0, "a wave's pieces are of known kinds");
 };
 
 template <int DH, int DV>
-__global__ void __launch_bounds__(64 * kWaves, DV == 128 ? 2 : 1) attend_kernel(AttendArgs a, int n_tiles) {
+__global__ void __launch_bounds__(64 * kWaves, (AttendTile<DH, DV>::kPerUnit)) attend_kernel(AttendArgs a, int n_tiles) {
   typedef AttendTile<DH, DV> Tile;
-  constexpr int DR = 64, KC = Tile::KC, KR = Tile::KR, MT = Tile::MT, NB = Tile::kBuffers, PIECES = Tile::kPieces;
+  constexpr int DR = 64, KC = Tile::KC, KR = Tile::KR, MT = Tile::MT, PIECES = Tile::kPieces;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -63,7 +64,12 @@ __global__ void __launch_bounds__(64 * kWaves, DV == 128 ? 2 : 1) attend_kernel(
   const int64_t cap = (int64_t)a.cache.max_pages * P;
   const int64_t p0 = (int64_t)r.len - r.n;                             // position of the sequence's first row
   auto visible = [&](int64_t rho) { return (int)min(max(p0 + rho / a.G + 1, (int64_t)0), cap); };   // tokens that a row sees
-  const int64_t rho0 = tile0 + wave * 32, last = rows - 1;
+  // Waves that would have no rows help the others: with at most 64 rows in the tile two teams, with at most 32 four, take the
+  // tiles of 32 tokens in turn and join their states at the end.
+  const int64_t last = rows - 1;
+  const int team_bits = last - tile0 < 32 ? 2 : last - tile0 < 64 ? 1 : 0, row_waves = kWaves >> team_bits;
+  const int team = wave >> (2 - team_bits), row_wave = wave & (row_waves - 1);
+  const int64_t rho0 = tile0 + row_wave * 32;
   const int64_t rho = min(rho0 + n, last);                             // rows behind the last repeat it and are not stored
   const int t = (int)(rho / a.G), head = j * a.G + (int)(rho % a.G);
   const int vis = visible(rho);
@@ -123,19 +129,20 @@ __global__ void __launch_bounds__(64 * kWaves, DV == 128 ? 2 : 1) attend_kernel(
 
   // Where this wave's pieces of a stage begin in a page (32 bits: the host has seen to that), for its first slots; a stage further on
   // in the page adds 64 vectors of 16 bytes to those of K and k_R, 64 * DV bytes to those of V.
-  uint32_t off[Tile::kPer];
+  const uint32_t off_k = (h * P + n) * 16, off_v = (n * 2 + h) * 16;   // this lane's vector of a piece
+  uint32_t piece_at[Tile::kPer];
 #pragma unroll
   for (int i = 0; i < Tile::kPer; ++i) {
     const int piece = wave + kWaves * i;                               // [kind][32-token tile][fragment]
     if (kWaves * i < 2 * KC) {
       const int tt = piece / KC, kp = piece % KC;
-      off[i] = ((j * (DH / 16) + 2 * kp + h) * P + 32 * tt + n) * 16;
+      piece_at[i] = ((j * (DH / 16) + 2 * kp) * P + 32 * tt) * 16;
     } else if (kWaves * i < 2 * (KC + KR)) {
       const int p = piece - 2 * KC, tt = p / KR, ks = p % KR;
-      off[i] = P * gc * (DH + DV) + ((2 * ks + h) * P + 32 * tt + n) * 16;
+      piece_at[i] = P * gc * (DH + DV) + (2 * ks * P + 32 * tt) * 16;
     } else {
       const int p = piece - 2 * (KC + KR), tt = p / MT, mt = p % MT;
-      off[i] = P * gc * DH + (((j * (P / 32) + tt) * DV + 32 * mt + n) * 2 + h) * 16;
+      piece_at[i] = P * gc * DH + ((j * (P / 32) + tt) * DV + 32 * mt) * 32;
     }
   }
   const uint32_t page_bytes = P * (gc * (DH + DV) + DR * 2) + gc * (P / 32) * 8;
@@ -165,7 +172,7 @@ __global__ void __launch_bounds__(64 * kWaves, DV == 128 ? 2 : 1) attend_kernel(
     for (int i = 0; i < Tile::kPer; ++i)
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                    :
-                   : "s"(lds + kWaves * i * 1024), "v"(off[i]), "s"(kWaves * i < 2 * (KC + KR) ? kr : v)
+                   : "s"(lds + kWaves * i * 1024), "v"(kWaves * i < 2 * (KC + KR) ? off_k : off_v), "s"((kWaves * i < 2 * (KC + KR) ? kr : v) + piece_at[i])
                    : "memory");
   };
   auto scales_of = [&](Stage g) -> f32x4 {                              // K, V of the stage's first tile, K, V of its second
@@ -194,21 +201,11 @@ __global__ void __launch_bounds__(64 * kWaves, DV == 128 ? 2 : 1) attend_kernel(
     }
 #pragma unroll
     for (int ks = 0; ks < KR; ++ks) s = mfma32(*(const bf16x8*)(r_lds + ks * 1024), qr[ks], s);
-    u32x4 v8[MT];
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) v8[mt] = *(const u32x4*)(v_lds + mt * 1024);
     // register i of lane (n, h): token tok + 8 (i / 4) + 4 h + i % 4
     if (tok + 32 > vis_min) {
 #pragma unroll
       for (int i = 0; i < 16; ++i)
         if (tok + 8 * (i >> 2) + 4 * h + (i & 3) >= vis) s[i] = GQLA_NEG_INF;
-      if (tok + 32 > vis_max) {   // codes of tokens that no row of the wave sees may be anything (NaN included)
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (tok + 16 * (e >> 3) + 8 * h + (e & 7) >= vis_max) v8[mt][e >> 2] &= ~(0xffu << (8 * (e & 3)));
-      }
     }
     float top = fmaxf(s[0], s[1]);
 #pragma unroll
@@ -245,47 +242,77 @@ __global__ void __launch_bounds__(64 * kWaves, DV == 128 ? 2 : 1) attend_kernel(
       pf[kk] = __builtin_bit_cast(bf16x8, w);
     }
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
+    for (int mt = 0; mt < MT; ++mt) {
+      const u32x4 v8 = *(const u32x4*)(v_lds + mt * 1024);
 #pragma unroll
-      for (int kk = 0; kk < 2; ++kk) o[mt] = mfma32(widen_codes(v8[mt][2 * kk], v8[mt][2 * kk + 1], sc_v), pf[kk], o[mt]);
+      for (int kk = 0; kk < 2; ++kk) o[mt] = mfma32(widen_codes(v8[2 * kk], v8[2 * kk + 1], sc_v), pf[kk], o[mt]);
+    }
   };
 
   if (st0 < st1) {
-    Stage g[NB];                                                       // this stage and those ahead
-#pragma unroll
-    for (int i = 0; i < NB; ++i) {
-      g[i] = Stage{-1, 0};
-      if (st0 + i < st1) g[i] = look_up();
-    }
-#pragma unroll
-    for (int i = 0; i < NB - 1; ++i)
-      if (st0 + i < st1) request(g[i], i);
-    f32x4 sc = scales_of(g[0]);
-    int buf = 0;
+    Stage here = look_up(), next = here;                               // this stage; the next one, looked up a stage ahead of its request
+    if (st0 + 1 < st1) next = look_up();
+    request(here, 0);
+    f32x4 sc = scales_of(here);
     for (int st = st0; st < st1; ++st) {
-      // this stage's requests are the oldest: those of the NB - 2 stages behind it may be on their way still
-      if (NB > 2 && st + 1 < st1) {
-        static_assert(NB == 2 || Tile::kPer == 6, "the wait is written for this count");
-        asm volatile("s_waitcnt vmcnt(6)" ::: "memory");
-      } else {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      }
-      __syncthreads();                                                 // every wave's share is there; the buffer before is free
-      if (st + NB - 1 < st1) request(g[NB - 1], buf == 0 ? NB - 1 : buf - 1);
-      const bool there = g[0].page >= 0;
-#pragma unroll
-      for (int i = 0; i + 1 < NB; ++i) g[i] = g[i + 1];
+      const int buf = (st - st0) & 1;
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();                                                 // every wave's share is there; the other buffer is free
+      if (st + 1 < st1) request(next, buf ^ 1);
+      const bool there = here.page >= 0;
+      here = next;
       const f32x4 now = sc;
-      if (st + 1 < st1) sc = scales_of(g[0]);
-      if (st + NB < st1) g[NB - 1] = look_up();
+      if (st + 1 < st1) sc = scales_of(here);
+      if (st + 2 < st1) next = look_up();
       const int tok = st * kStage;
+      if (there && r.len - tok < kStage) {   // the sequence ends here: value codes behind it may be anything (NaN included), a weight of 0 is not enough
+        char* vectors = smem + (buf * PIECES + 2 * (KC + KR)) * 1024 + lane * 16;
+        for (int p = wave; p < 2 * MT; p += kWaves) {
+          u32x4 v = *(const u32x4*)(vectors + p * 1024);
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (tok + p / MT * 32 + 16 * (e >> 3) + 8 * h + (e & 7) >= r.len) v[e >> 2] &= ~(0xffu << (8 * (e & 3)));
+          *(u32x4*)(vectors + p * 1024) = v;
+        }
+        __syncthreads();
+      }
       if (there) {                                                     // a page that is not there holds nothing
         const char* lds = smem + buf * (PIECES * 1024) + lane * 16;
-        if (tok < vis_max) attend_tile(tok, lds, lds + 2 * KC * 1024, lds + 2 * (KC + KR) * 1024, now[0], now[1]);
-        if (tok + 32 < vis_max)
+        // tile q of 32 tokens is team q mod teams's
+        const int teams = 1 << team_bits, first = 2 * st & (teams - 1);
+        if (tok < vis_max && team == first) attend_tile(tok, lds, lds + 2 * KC * 1024, lds + 2 * (KC + KR) * 1024, now[0], now[1]);
+        if (tok + 32 < vis_max && team == (first + 1 & (teams - 1)))
           attend_tile(tok + 32, lds + KC * 1024, lds + (2 * KC + KR) * 1024, lds + (2 * (KC + KR) + MT) * 1024, now[2], now[3]);
       }
-      buf = buf == NB - 1 ? 0 : buf + 1;
+    }
+  }
+  // the teams' states become one, half of them at a time
+  for (int half = 1 << team_bits >> 1; half > 0; half >>= 1) {
+    __syncthreads();                                                   // the ring, then the states before, are no longer read
+    char* const state = smem + ((team & (half - 1)) * row_waves + row_wave) * Tile::kState;
+    if (team >= half && team < 2 * half) {
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) *(f32x4*)(state + ((mt * 4 + q) * 64 + lane) * 16) = f32x4{o[mt][4 * q], o[mt][4 * q + 1], o[mt][4 * q + 2], o[mt][4 * q + 3]};
+      *(float*)(state + MT * 4096 + lane * 4) = m_run;
+      *(float*)(state + MT * 4096 + 256 + lane * 4) = l_run;
+    }
+    __syncthreads();
+    if (team < half) {
+      const float m_other = *(const float*)(state + MT * 4096 + lane * 4), l_other = *(const float*)(state + MT * 4096 + 256 + lane * 4);
+      const float m_new = fmaxf(m_run, m_other), m_use = m_new == GQLA_NEG_INF ? 0.f : m_new;
+      const float mine = fast_exp2(m_run - m_use), other = fast_exp2(m_other - m_use);
+      m_run = m_new;
+      l_run = l_run * mine + l_other * other;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const f32x4 x = *(const f32x4*)(state + ((mt * 4 + q) * 64 + lane) * 16);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[mt][4 * q + i] = o[mt][4 * q + i] * mine + x[i] * other;
+        }
     }
   }
 
@@ -296,8 +323,9 @@ __global__ void __launch_bounds__(64 * kWaves, DV == 128 ? 2 : 1) attend_kernel(
   const int64_t at = row * a.h_q + head;
   if (a.splits == 1) {
     // through LDS, so that rows leave as runs of 16-byte vectors
-    __syncthreads();                                                   // the ring is no longer read
-    char* const mine = smem + wave * (32 * Tile::kPitch);
+    __syncthreads();                                                   // the ring (or a state) is no longer read
+    if (team > 0) return;
+    char* const mine = smem + row_wave * (32 * Tile::kPitch);
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -315,42 +343,85 @@ __global__ void __launch_bounds__(64 * kWaves, DV == 128 ? 2 : 1) attend_kernel(
       const int64_t to = ((int64_t)r.first + t_first + dt) * a.h_q + j * a.G + (k - dt * a.G);
       *(u32x4*)((__bf16*)a.out + to * DV + 8 * c) = *(const u32x4*)(mine + nr * Tile::kPitch + c * 16);
     }
-  } else if (row_ok) {
+  } else if (row_ok && team == 0) {
     const int64_t part = (int64_t)split * a.total * a.h_q + at;
+    if (h == 0) a.part_lse[part] = lse;
+    if (st0 >= st1) return;                                            // (nothing in this range: the weight of -inf is 0)
     float* po = a.part_o + part * DV + 4 * h;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
       for (int q = 0; q < 4; ++q)
         *(f32x4*)(po + 32 * mt + 8 * q) = f32x4{o[mt][4 * q] * inv, o[mt][4 * q + 1] * inv, o[mt][4 * q + 2] * inv, o[mt][4 * q + 3] * inv};
-    if (h == 0) a.part_lse[part] = lse;
   }
 }
 
-// Merge of the splits: DV / 4 threads per row, rows of sequences only (packed rows behind the last sequence stay as they are).
+// Joins the splits' partial outputs.  DV / 4 threads hold a row's vectors; as many slices of the splits as a workgroup has room for
+// (slices, a power of two) are merged side by side, each with a running maximum, and meet in LDS.  Rows of sequences only:
+// packed rows behind the last one stay as they are.
 template <int DV>
-__global__ void __launch_bounds__(256) attend_merge_kernel(AttendArgs a) {
-  constexpr int VEC = DV / 4;
+__global__ void __launch_bounds__(256) attend_merge_kernel(AttendArgs a, int slices) {
+  constexpr int VEC = DV / 4, GROUPS = 256 / VEC, AT_ONCE = 4;
+  __shared__ f32x4 acc_lds[GROUPS][VEC];
+  __shared__ float m_lds[GROUPS], den_lds[GROUPS];
   const int64_t rows = (int64_t)a.total * a.h_q;
-  const int64_t at = (int64_t)blockIdx.x * (256 / VEC) + threadIdx.x / VEC;
-  const int v = threadIdx.x % VEC;
-  if (at >= rows) return;
-  const int row = (int)(at / a.h_q);
+  const int group = threadIdx.x / VEC, v = threadIdx.x % VEC, slice = group & (slices - 1);
+  const int64_t at = (int64_t)blockIdx.x * (GROUPS / slices) + group / slices;
   const int begin = a.first ? min(max(a.first[0], 0), a.total) : 0, end = a.first ? min(max(a.first[a.B], 0), a.total) : a.total;
-  if (row < begin || row >= end) return;
-  float m = GQLA_NEG_INF;
-  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.part_lse[s * rows + at]);
-  const float m_use = m == GQLA_NEG_INF ? 0.f : m;
-  float den = 0.f;
+  const bool ok = at >= (int64_t)begin * a.h_q && at < (int64_t)end * a.h_q;
+  float m = GQLA_NEG_INF, den = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < a.splits; ++s) {
-    const float w = __expf(a.part_lse[s * rows + at] - m_use);
-    den += w;
-    if (w > 0.f) acc += w * *(const f32x4*)(a.part_o + (s * rows + at) * DV + 4 * v);
+  if (ok) {
+    for (int s = slice; s < a.splits; s += AT_ONCE * slices) {
+      float l[AT_ONCE];
+      f32x4 x[AT_ONCE];
+#pragma unroll
+      for (int u = 0; u < AT_ONCE; ++u) {
+        const int su = s + u * slices;
+        l[u] = GQLA_NEG_INF;
+        x[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (su < a.splits) l[u] = a.part_lse[su * rows + at];
+      }
+#pragma unroll
+      for (int u = 0; u < AT_ONCE; ++u)
+        if (l[u] != GQLA_NEG_INF) x[u] = *(const f32x4*)(a.part_o + ((s + u * slices) * rows + at) * DV + 4 * v);
+      float m_new = m;
+#pragma unroll
+      for (int u = 0; u < AT_ONCE; ++u) m_new = fmaxf(m_new, l[u]);
+      const float m_use = m_new == GQLA_NEG_INF ? 0.f : m_new, old = __expf(m - m_use);
+      m = m_new;
+      den *= old;
+      acc *= old;
+#pragma unroll
+      for (int u = 0; u < AT_ONCE; ++u) {
+        const float w = __expf(l[u] - m_use);
+        den += w;
+        acc += w * x[u];
+      }
+    }
   }
-  const float inv = den > 0.f ? 1.f / den : 0.f;
+  if (slices > 1) {
+    acc_lds[group][v] = acc;
+    if (v == 0) {
+      m_lds[group] = m;
+      den_lds[group] = den;
+    }
+    __syncthreads();
+    if (slice > 0) return;
+    for (int s = 1; s < slices; ++s) m = fmaxf(m, m_lds[group + s]);
+    const float m_use = m == GQLA_NEG_INF ? 0.f : m, mine = __expf(m_lds[group] - m_use);
+    den *= mine;
+    acc *= mine;
+    for (int s = 1; s < slices; ++s) {
+      const float w = __expf(m_lds[group + s] - m_use);
+      den += w * den_lds[group + s];
+      acc += w * acc_lds[group + s][v];
+    }
+  }
+  if (!ok) return;
+  const float inv = den == 0.f ? 0.f : 1.f / den;
   *(u32x2*)((__bf16*)a.out + at * DV + 4 * v) = u32x2{pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv)};
-  if (a.lse && v == 0) a.lse[at] = m + __logf(den);
+  if (a.lse && v == 0) a.lse[at] = den == 0.f ? GQLA_NEG_INF : m + __logf(den);
 }
 
 // Dynamic LDS beyond 64 KB has to be allowed once per kernel and device.
@@ -376,19 +447,21 @@ hipError_t launch_attend(const AttendArgs& a, hipStream_t s) {
   attend_kernel<DH, DV><<<(unsigned)(tiles * a.g * a.splits), 64 * kWaves, kLds, s>>>(a, (int)tiles);
   e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
-  const int per = 256 / (DV / 4);
-  attend_merge_kernel<DV><<<(unsigned)(((int64_t)a.total * a.h_q + per - 1) / per), 256, 0, s>>>(a);
+  int slices = 1;
+  while (2 * slices <= a.splits && 2 * slices <= 256 / (DV / 4)) slices *= 2;
+  const int per = 256 / (DV / 4) / slices;
+  attend_merge_kernel<DV><<<(unsigned)(((int64_t)a.total * a.h_q + per - 1) / per), 256, 0, s>>>(a, slices);
   return hipGetLastError();
 }
 
 }  // namespace
 
-// Ranges of the context: as many as leave the chip's 256 units with about two workgroups each, none shorter than 256 tokens.
+// Ranges of the context: as many as the chip's 256 units have room for (with as many rows in every sequence; ragged ones may need a
+// tile more each), none shorter than 256 tokens.
 int attend_splits(int64_t total, int64_t batch, int h_q, int g, int d_h, int64_t max_tokens) {
-  (void)d_h;
-  const int64_t groups = row_runs(total, h_q / g, kRows, 1, batch) * g;
-  const int64_t want = (512 + groups - 1) / groups, most = (max_tokens + 255) / 256;
-  return (int)std::max<int64_t>(1, std::min<int64_t>({want, most, 64}));
+  const int64_t room = 256 * (d_h == 192 ? AttendTile<192, 256>::kPerUnit : AttendTile<128, 128>::kPerUnit);
+  const int64_t rows = total * (h_q / g), tiles = batch * ((rows + batch * kRows - 1) / (batch * kRows)) * g;
+  return (int)std::max<int64_t>(1, std::min<int64_t>({room / std::max<int64_t>(tiles, 1), (max_tokens + 255) / 256, 64}));
 }
 
 hipError_t launch_attend_fp8_blocks(const AttendArgs& a, hipStream_t s) {
