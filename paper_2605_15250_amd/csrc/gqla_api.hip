@@ -964,6 +964,7 @@ gqla_status gqla_attend_gqa_fp8_blocks(const gqla_shape* shape, const int32_t* f
   if (shape->batch == 0 || total == 0) return GQLA_OK;
   AttendArgs a;
   a.G = shape->h_q / shape->g;
+  a.by_G = make_divisor((uint32_t)a.G);
   a.splits = attend_splits_of(shape, total, expanded_blocks);
   // offsets inside a page are 32-bit
   if (gqla_expanded_fp8_blocks_page_bytes(shape->g, shape->d_h, value_dim(shape), shape->d_r, expanded_blocks->page_size) > INT32_MAX)

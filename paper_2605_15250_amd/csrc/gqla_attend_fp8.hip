@@ -58,21 +58,22 @@ __global__ void __launch_bounds__(64 * kWaves, (AttendTile<DH, DV>::kPerUnit)) a
   const int j = blockIdx.x % a.g, split = blockIdx.x / a.g % a.splits, tile = n_tiles - 1 - (int)(blockIdx.x / (a.g * a.splits));
   RowSpan r;
   if (!find_rows<kRows, 1>(a.first, a.seq_lens, a.B, a.total, a.s_q, a.G, tile, r)) return;
-  const int64_t rows = (int64_t)r.n * a.G, tile0 = (int64_t)r.k * kRows;
+  const int rows = r.n * a.G, tile0 = r.k * kRows;                     // (the host has seen to 32 bits)
   if (tile0 >= rows) return;
   const int P = a.cache.page_size, gc = a.g;
   const int64_t cap = (int64_t)a.cache.max_pages * P;
-  const int64_t p0 = (int64_t)r.len - r.n;                             // position of the sequence's first row
-  auto visible = [&](int64_t rho) { return (int)min(max(p0 + rho / a.G + 1, (int64_t)0), cap); };   // tokens that a row sees
+  auto token = [&](int rho) { return (int)a.by_G(rho); };              // of the sequence's rows
+  const int before = r.len - r.n;                                      // tokens ahead of the sequence's first row
+  auto visible = [&](int rho) { return (int)min((int64_t)max(before + token(rho) + 1, 0), cap); };   // tokens that a row sees
   // Waves that would have no rows help the others: with at most 64 rows in the tile two teams, with at most 32 four, take the
   // tiles of 32 tokens in turn and join their states at the end.
-  const int64_t last = rows - 1;
+  const int last = rows - 1;
   const int team_bits = last - tile0 < 32 ? 2 : last - tile0 < 64 ? 1 : 0, row_waves = kWaves >> team_bits;
   const int team = wave >> (2 - team_bits), row_wave = wave & (row_waves - 1);
-  const int64_t rho0 = tile0 + row_wave * 32;
-  const int64_t rho = min(rho0 + n, last);                             // rows behind the last repeat it and are not stored
-  const int t = (int)(rho / a.G), head = j * a.G + (int)(rho % a.G);
-  const int vis = visible(rho);
+  const int rho0 = tile0 + row_wave * 32;
+  const int rho = min(rho0 + n, last);                                 // rows behind the last repeat it and are not stored
+  const int t = token(rho), head = j * a.G + rho - t * a.G;
+  const int vis = (int)min((int64_t)max(before + t + 1, 0), cap);
   const int vis_min = visible(min(rho0, last)), vis_max = visible(min(rho0 + 31, last));   // of the wave
   const int stages = (int)(((int64_t)visible(min(tile0 + kRows - 1, last)) + kStage - 1) / kStage);
   const int per = (stages + a.splits - 1) / a.splits;
@@ -185,8 +186,11 @@ __global__ void __launch_bounds__(64 * kWaves, (AttendTile<DH, DV>::kPerUnit)) a
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[mt][i] = 0.f;
   float m_run = GQLA_NEG_INF, l_run = 0.f;
+  const int key_lane = (32 * h + (n & 19) + ((n & 4) << 1) + ((n & 8) >> 1)) * 16;
 
-  // 32 tokens from `tok` on, whose pieces begin at lds (k_R and V behind the K pieces of both tiles)
+  // 32 tokens from `tok` on, whose pieces begin at lds (k_R and V behind the K pieces of both tiles).  Lane n takes the keys of token
+  // n with bits 2 and 3 exchanged: register i of the scores in lane (n, h) is then token 16 (i / 8) + 8 h + i % 8, which is the token
+  // order of the other operand's fragments, and probabilities need no exchange between the half-waves.
   auto attend_tile = [&](int tok, const char* k_lds, const char* r_lds, const char* v_lds, float sc_k, float sc_v) __attribute__((always_inline)) {
     f32x16 s;
 #pragma unroll
@@ -201,18 +205,16 @@ __global__ void __launch_bounds__(64 * kWaves, (AttendTile<DH, DV>::kPerUnit)) a
     }
 #pragma unroll
     for (int ks = 0; ks < KR; ++ks) s = mfma32(*(const bf16x8*)(r_lds + ks * 1024), qr[ks], s);
-    // register i of lane (n, h): token tok + 8 (i / 4) + 4 h + i % 4
     if (tok + 32 > vis_min) {
 #pragma unroll
       for (int i = 0; i < 16; ++i)
-        if (tok + 8 * (i >> 2) + 4 * h + (i & 3) >= vis) s[i] = GQLA_NEG_INF;
+        if (tok + 16 * (i >> 3) + 8 * h + (i & 7) >= vis) s[i] = GQLA_NEG_INF;
     }
     float top = fmaxf(s[0], s[1]);
 #pragma unroll
     for (int i = 2; i < 16; i += 2) top = fmaxf(fmaxf(top, s[i]), s[i + 1]);
-    top = pair_max(top) * a.scale_log2e;
-    if (__builtin_amdgcn_ballot_w64(top > m_run + kRescale) != 0) {
-      const float m_new = fmaxf(m_run, top);
+    if (__builtin_amdgcn_ballot_w64(top * a.scale_log2e > m_run + kRescale) != 0) {
+      const float m_new = fmaxf(m_run, pair_max(top) * a.scale_log2e);
       const float alpha = fast_exp2(m_run - (m_new == GQLA_NEG_INF ? 0.f : m_new));
       m_run = m_new;
       l_run *= alpha;
@@ -231,14 +233,8 @@ __global__ void __launch_bounds__(64 * kWaves, (AttendTile<DH, DV>::kPerUnit)) a
     bf16x8 pf[2];
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk) {
-      u32x4 w;
-      uint32_t r0, r1;
-      half_swap(pack_bf16(p[8 * kk], p[8 * kk + 1]), pack_bf16(p[8 * kk + 4], p[8 * kk + 5]), r0, r1);
-      w[0] = r0;
-      w[2] = r1;
-      half_swap(pack_bf16(p[8 * kk + 2], p[8 * kk + 3]), pack_bf16(p[8 * kk + 6], p[8 * kk + 7]), r0, r1);
-      w[1] = r0;
-      w[3] = r1;
+      const u32x4 w = {pack_bf16(p[8 * kk], p[8 * kk + 1]), pack_bf16(p[8 * kk + 2], p[8 * kk + 3]),
+                       pack_bf16(p[8 * kk + 4], p[8 * kk + 5]), pack_bf16(p[8 * kk + 6], p[8 * kk + 7])};
       pf[kk] = __builtin_bit_cast(bf16x8, w);
     }
 #pragma unroll
@@ -277,12 +273,12 @@ __global__ void __launch_bounds__(64 * kWaves, (AttendTile<DH, DV>::kPerUnit)) a
         __syncthreads();
       }
       if (there) {                                                     // a page that is not there holds nothing
-        const char* lds = smem + buf * (PIECES * 1024) + lane * 16;
+        const char *ring = smem + buf * (PIECES * 1024), *keys = ring + key_lane, *vals = ring + 2 * (KC + KR) * 1024 + lane * 16;
         // tile q of 32 tokens is team q mod teams's
         const int teams = 1 << team_bits, first = 2 * st & (teams - 1);
-        if (tok < vis_max && team == first) attend_tile(tok, lds, lds + 2 * KC * 1024, lds + 2 * (KC + KR) * 1024, now[0], now[1]);
+        if (tok < vis_max && team == first) attend_tile(tok, keys, keys + 2 * KC * 1024, vals, now[0], now[1]);
         if (tok + 32 < vis_max && team == (first + 1 & (teams - 1)))
-          attend_tile(tok + 32, lds + KC * 1024, lds + (2 * KC + KR) * 1024, lds + (2 * (KC + KR) + MT) * 1024, now[2], now[3]);
+          attend_tile(tok + 32, keys + KC * 1024, keys + (2 * KC + KR) * 1024, vals + MT * 1024, now[2], now[3]);
       }
     }
   }
@@ -334,13 +330,12 @@ __global__ void __launch_bounds__(64 * kWaves, (AttendTile<DH, DV>::kPerUnit)) a
             u32x2{pack_bf16(o[mt][4 * q] * inv, o[mt][4 * q + 1] * inv), pack_bf16(o[mt][4 * q + 2] * inv, o[mt][4 * q + 3] * inv)};
     if (a.lse && h == 0 && row_ok) a.lse[at] = lse;
     constexpr int LPR = DV / 8;                                        // lanes per row
-    const int t_first = (int)(min(rho0, last) / a.G), rest = (int)(min(rho0, last) % a.G);
 #pragma unroll
     for (int i = 0; i < 32 * LPR / 64; ++i) {
       const int nr = (i * 64 + lane) / LPR, c = lane % LPR;
       if (rho0 + nr > last) continue;
-      const uint32_t k = (uint32_t)(rest + nr), dt = k / (uint32_t)a.G;
-      const int64_t to = ((int64_t)r.first + t_first + dt) * a.h_q + j * a.G + (k - dt * a.G);
+      const int tk = token(rho0 + nr);
+      const int64_t to = ((int64_t)r.first + tk) * a.h_q + j * a.G + (rho0 + nr - tk * a.G);
       *(u32x4*)((__bf16*)a.out + to * DV + 8 * c) = *(const u32x4*)(mine + nr * Tile::kPitch + c * 16);
     }
   } else if (row_ok && team == 0) {

@@ -98,6 +98,18 @@ struct AppendRowsArgs {
   int32_t B, total, s_q, h_q, g, d_h, d_v, d_r;
 };
 
+// Division of 31-bit numbers by a constant of the launch: floor(x / d) = (x * m) >> s with m = ceil(2^s / d), s = 31 + ceil(log2 d), exact as
+// m d - 2^s < d <= 2^(s - 31) and x < 2^31.
+struct Divisor {
+  uint32_t m, s;
+  __host__ __device__ uint32_t operator()(uint32_t x) const { return (uint32_t)((uint64_t)x * m >> s); }
+};
+inline Divisor make_divisor(uint32_t d) {
+  uint32_t s = 31;
+  while ((1ull << (s - 31)) < d) ++s;
+  return Divisor{(uint32_t)(((1ull << s) + d - 1) / d), s};
+}
+
 struct AttendArgs {
   const void *q_c, *q_r;            // packed rows [total][h_q][..]
   void* out;
@@ -108,6 +120,7 @@ struct AttendArgs {
   float* part_o;                    // splits > 1: [splits][total][h_q][d_v], then the log-sum-exps [splits][total][h_q]
   float* part_lse;
   int32_t B, total, s_q, h_q, g, G, d_h, d_v, splits;
+  Divisor by_G;                     // G = h_q / g
   float scale_log2e;
 };
 
