@@ -14,6 +14,7 @@
 // Few rows over a long context: the tokens are split into ranges, whose partial outputs a second kernel joins.
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 
 #include "gqla_lds.h"
 #include "gqla_rows.h"
@@ -41,21 +42,34 @@ struct AttendTile {
   static constexpr int kPieces = 2 * (KC + KR + MT), kPer = kPieces / kWaves;
   static constexpr int kPitch = DV * 2 + 16;                           // of an output row on its way through LDS
   static constexpr int kState = MT * 4096 + 512;                       // a wave's O^T, maxima and sums on their way to another wave
-  static constexpr int kPerUnit = DV == 128 ? 3 : 2;                   // workgroups of a compute unit (registers; three rings of 48 KB)
+  // Workgroups of a compute unit: registers allow three (two with value dims of 256), and two stages in the ring leave LDS for them.
+  // (Three stages and two workgroups: a few rows over 20000 to 32000 tokens 41 us as well, 64 sequences of 2500 to 5000 158 us instead of 125.)
+  static constexpr int kPerUnit = DV == 128 ? 3 : 2;
   static constexpr int kLds = std::max(2 * kPieces * 1024, std::max(kRows * kPitch, 2 * kState));
   static_assert(2 * KC % kWaves == 0 && 2 * KR % kWaves == 0 && 2 * MT % kWaves == 0, "a wave's pieces are of known kinds");
 };
 
 template <int DH, int DV>
-__global__ void __launch_bounds__(64 * kWaves, (AttendTile<DH, DV>::kPerUnit)) attend_kernel(AttendArgs a, int n_tiles) {
+__global__ void __launch_bounds__(64 * kWaves, (AttendTile<DH, DV>::kPerUnit)) attend_kernel(AttendArgs a, int n_tiles, int spread) {
   typedef AttendTile<DH, DV> Tile;
   constexpr int DR = 64, KC = Tile::KC, KR = Tile::KR, MT = Tile::MT, PIECES = Tile::kPieces;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // (workgroups go to the eight dies in turn: with g a multiple or a divisor of 8 a die keeps to its groups' keys and values; the
-  // tiles with the most tokens in sight come first)
-  const int j = blockIdx.x % a.g, split = blockIdx.x / a.g % a.splits, tile = n_tiles - 1 - (int)(blockIdx.x / (a.g * a.splits));
+  // Workgroups go to the eight dies in turn.  Many tiles of rows a sequence: with g a multiple or a divisor of 8 a die keeps to its groups'
+  // keys and values, which its L2 then holds for all of them; the tiles with the most tokens in sight come first.  One tile (spread):
+  // the groups of a (tile, range) stay on one die, for the k_R that they share.
+  int j, unit;
+  if (spread) {
+    const int k = blockIdx.x >> 3;
+    j = k % a.g;
+    unit = k / a.g * 8 + (blockIdx.x & 7);
+    if (unit >= n_tiles * a.splits) return;
+  } else {
+    j = blockIdx.x % a.g;
+    unit = blockIdx.x / a.g;
+  }
+  const int split = unit % a.splits, tile = n_tiles - 1 - unit / a.splits;
   RowSpan r;
   if (!find_rows<kRows, 1>(a.first, a.seq_lens, a.B, a.total, a.s_q, a.G, tile, r)) return;
   const int rows = r.n * a.G, tile0 = r.k * kRows;                     // (the host has seen to 32 bits)
@@ -433,13 +447,17 @@ hipError_t allow_lds() {
   return e;
 }
 
+// tiles of rows of a sequence, if all have as many
+int64_t sequence_tiles(int64_t total, int64_t batch, int64_t G) { return std::max<int64_t>(1, (total * G + batch * kRows - 1) / (batch * kRows)); }
+
 template <int DH, int DV>
 hipError_t launch_attend(const AttendArgs& a, hipStream_t s) {
-  constexpr int kLds = AttendTile<DH, DV>::kLds;
   hipError_t e = allow_lds<DH, DV>();
   if (e != hipSuccess) return e;
-  const int64_t tiles = row_runs(a.total, a.G, kRows, 1, a.B);
-  attend_kernel<DH, DV><<<(unsigned)(tiles * a.g * a.splits), 64 * kWaves, kLds, s>>>(a, (int)tiles);
+  const int64_t tiles = row_runs(a.total, a.G, kRows, 1, a.B), units = tiles * a.splits;
+  // (spread: 64 sequences of 2500 to 5000 tokens, 8 groups, 4 to 8 rows of 4 heads each: 138 -> 123 us; 32 of 4000 to 6000, 4 rows of 16: 101 -> 93)
+  const bool spread = sequence_tiles(a.total, a.B, a.G) == 1;
+  attend_kernel<DH, DV><<<(unsigned)((spread ? (units + 7) / 8 * 8 : units) * a.g), 64 * kWaves, AttendTile<DH, DV>::kLds, s>>>(a, (int)tiles, spread);
   e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
   int slices = 1;
@@ -451,12 +469,36 @@ hipError_t launch_attend(const AttendArgs& a, hipStream_t s) {
 
 }  // namespace
 
-// Ranges of the context: as many as the chip's 256 units have room for (with as many rows in every sequence; ragged ones may need a
-// tile more each), none shorter than 256 tokens.
+// Ranges that the tokens are split into: the number with the smallest time by this model, in microseconds, of the 256 units:
+//   N = groups * tiles * splits workgroups of ceil(stages / splits) stages each (two more for their start and end);
+//   a stage takes a workgroup `stage[k]` times the k workgroups that share its unit: up to k = 1, 2, 3 on each unit when N is at most 256 k,
+//   beyond that all run in turn, with half a turn in which units run out of work;
+//   a merge costs 5 us and the partial outputs, written and read at 2.4 TB/s.
+// The rates are fits to sweeps of 1 to 96 ranges.  (time of the call with 1, the chosen number and twice as many) 9 to 16 rows of 4 heads over
+// 20000 to 32000 tokens, 2 sequences: 520, 41 (32), 48 us; 32 sequences of 4000 to 6000, 4 rows of 16 heads: 139, 93 (3), 107; 8 of
+// 10000 to 20000: 399, 99 (12), 115; 8 chunks of 100 to 200 over 2500 to 5000: 157, 141 (2), 153; the same without a context: 24 (1), 40;
+// 1 prompt of 1000: 35 (1), 39.
 int attend_splits(int64_t total, int64_t batch, int h_q, int g, int d_h, int64_t max_tokens) {
-  const int64_t room = 256 * (d_h == 192 ? AttendTile<192, 256>::kPerUnit : AttendTile<128, 128>::kPerUnit);
-  const int64_t rows = total * (h_q / g), tiles = batch * ((rows + batch * kRows - 1) / (batch * kRows)) * g;
-  return (int)std::max<int64_t>(1, std::min<int64_t>({room / std::max<int64_t>(tiles, 1), (max_tokens + 255) / 256, 64}));
+  const int64_t G = h_q / g, tiles = sequence_tiles(total, batch, G) * batch * g;
+  const bool teams = total * G <= 64 * batch;                          // waves share a tile of rows
+  const int per_unit = d_h == 192 ? 2 : 3;
+  static constexpr double kStageTime[3][3] = {{1.8, 1.45, 1.35}, {1.7, 1.25, 1.15}, {2.4, 1.6, 0}};
+  const double* stage = kStageTime[d_h == 192 ? 2 : teams ? 1 : 0];
+  const double part_us = (double)total * h_q * (d_h == 192 ? 256 : 128) * 4 / 2.4e6;
+  const int64_t stages = (max_tokens + kStage - 1) / kStage;
+  int best = 1;
+  double best_us = 0;
+  for (int s = 1; s <= 64 && s <= stages; ++s) {
+    const double n = (double)tiles * s, length = (double)((stages + s - 1) / s + 2);
+    const int k = n >= 256.0 * per_unit ? per_unit : std::max(1, (int)std::ceil(n / 256.0));
+    double us = length * stage[k - 1] * (n > 256.0 * per_unit ? n / 256.0 + 0.5 * per_unit : k);
+    if (s > 1) us += 5 + s * part_us;
+    if (s == 1 || us < best_us) {
+      best = s;
+      best_us = us;
+    }
+  }
+  return best;
 }
 
 hipError_t launch_attend_fp8_blocks(const AttendArgs& a, hipStream_t s) {
