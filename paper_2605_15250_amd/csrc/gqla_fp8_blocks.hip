@@ -101,17 +101,23 @@ __device__ __forceinline__ uint32_t token_bytes(int w, int h, int a, int b) {
 // One wave per (sequence, block of 32 positions, group, K or V): it alone owns what it writes, its scale included, so there is
 // nothing to synchronise.  K: a lane takes one token and every second run of 8 dims, which are output vectors as they are.  V: a lane takes
 // 4 dims (8 with a value dim of 256) and the 16 tokens of an output vector, so that a load covers whole rows of two tokens and the turn from
-// token-major to dim-major happens in registers.  Rows of few tokens are stored byte by byte into their vectors (no read of what is
-// there); where the block holds older tokens and its exponent grows, vectors are read, rescaled and written back.
-// Four more workgroups per block take 8 tokens each and rotate: one sine and cosine per (token, pair) in LDS, shared by k_R and all
+// token-major to dim-major happens in registers; vectors that others share are stored element by element or, as codes, read, changed and
+// written back.  At most four new tokens (a step): a lane takes four dims of each, and codes are stored byte by byte, with no read of
+// what is there; only where the block's older codes need a larger exponent is this the long way again.
+// More workgroups per block take 8 tokens each, or 2, and rotate: one sine and cosine per (token, pair) in LDS, shared by k_R and all
 // heads of the queries; the angle is formed and reduced in double.
-// Bound by HBM for prompts and by latency for a step: a chain of row bounds and lengths -> page -> old scale -> stores.
+// Bound by HBM for prompts and by latency for a step: row bounds and lengths -> page (the rows on their way beside it) -> old scale -> stores.
+constexpr int kFew = 4;
+
 template <int DH, int DV, bool BLOCKS>
-__global__ void __launch_bounds__(256) append_rows_kernel(AppendRowsArgs a, int kv_groups) {
+__global__ void __launch_bounds__(256) append_rows_kernel(AppendRowsArgs a, int kv_groups, int turns_at_once) {
   constexpr int DR = 64;
   __shared__ float cs_tab[8 * DR];   // rotation: (cos, sin) of 8 tokens x 32 pairs
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const bool rotates = (int)blockIdx.y >= kv_groups;
+  double theta = 0.0;
+  if (rotates && a.log2_base > 0.0) theta = exp2(-2.0 * (int)(threadIdx.x & 31) / DR * a.log2_base) * 0.15915494309189535;
   RowSpan r;
   if (!find_rows<kBlock, 2>(a.first, a.seq_lens, a.B, a.total, a.s_q, 1, blockIdx.x, r)) return;
   // positions p0 .. len - 1 are new; this block's share is [lo, hi)
@@ -121,21 +127,24 @@ __global__ void __launch_bounds__(256) append_rows_kernel(AppendRowsArgs a, int 
   const int t0 = (int)t0_wide;
   const int P = a.cache.page_size;
   const int lo = (int)max((int64_t)t0, p0), hi = (int)min((int64_t)t0 + kBlock, (int64_t)r.len);
-  const int32_t pg = page_of_uniform(a.cache, r.b, t0 / P);
   const int slot0 = t0 % P, T = slot0 / kBlock, gc = a.g;
   constexpr int EB = BLOCKS ? 1 : 2;
   const int64_t page_bytes = (int64_t)P * (gc * (DH + DV) * EB + DR * 2) + (BLOCKS ? (int64_t)gc * (P / kBlock) * 8 : 0);
-  char* const page = (char*)a.cache.pool + (int64_t)(pg >= 0 ? pg : 0) * page_bytes;
+  auto look_up = [&](char*& page) {   // false: there is no such page
+    const int32_t pg = page_of_uniform(a.cache, r.b, t0 / P);
+    page = (char*)a.cache.pool + (int64_t)max(pg, 0) * page_bytes;
+    return pg >= 0;
+  };
+  char* page;
 
-  if ((int)blockIdx.y >= kv_groups) {   // rotation of 8 tokens
-    const int s0 = t0 + 8 * ((int)blockIdx.y - kv_groups);
-    const int first_t = max(s0, lo), last_t = min(s0 + 8, hi);
+  if (rotates) {   // turns_at_once tokens
+    const int s0 = t0 + turns_at_once * ((int)blockIdx.y - kv_groups);
+    const int first_t = max(s0, lo), last_t = min(s0 + turns_at_once, hi);
     if (first_t >= last_t) return;
-    const int tid = threadIdx.x, tok = tid >> 5, pair = tid & 31;
+    const int tid = threadIdx.x, tok = tid >> 5;
     float sn = 0.f, cs = 1.f;
-    if (a.log2_base > 0.0) {
-      const double theta = exp2(-2.0 * pair / DR * a.log2_base);
-      double turns = (double)(s0 + tok) * theta * 0.15915494309189535;
+    if (a.log2_base > 0.0 && tok < turns_at_once) {
+      double turns = (double)(s0 + tok) * theta;
       turns -= floor(turns);
       sincospif(2.0f * (float)turns, &sn, &cs);
     }
@@ -148,12 +157,6 @@ __global__ void __launch_bounds__(256) append_rows_kernel(AppendRowsArgs a, int 
     };
     const int64_t row0 = r.first + (first_t - p0);
     const int count = last_t - first_t, skip = first_t - s0;
-    if (tid < 8 * count && pg >= 0) {
-      const int i = tid >> 3, c = tid & 7;
-      const u32x4 v = *(const u32x4*)((const char*)a.k_r + ((row0 + i) * a.kr_stride + 8 * c) * 2);
-      char* const plane = page + (int64_t)P * gc * (DH + DV) * EB;
-      *(u32x4*)(plane + ((int64_t)c * P + slot0 + first_t - t0 + i) * 16) = a.log2_base > 0.0 ? turn(v, (skip + i) * 32 + 4 * c) : v;
-    }
     if (a.q_r) {
       const int per_token = a.h_q * 8, vecs = count * per_token;   // 16-byte vectors
       const u32x4* src = (const u32x4*)a.q_r + row0 * per_token;
@@ -170,31 +173,96 @@ __global__ void __launch_bounds__(256) append_rows_kernel(AppendRowsArgs a, int 
         }
       }
     }
+    if (tid < 8 * count && look_up(page)) {
+      const int i = tid >> 3, c = tid & 7;
+      const u32x4 v = *(const u32x4*)((const char*)a.k_r + ((row0 + i) * a.kr_stride + 8 * c) * 2);
+      char* const plane = page + (int64_t)P * gc * (DH + DV) * EB;
+      *(u32x4*)(plane + ((int64_t)c * P + slot0 + first_t - t0 + i) * 16) = a.log2_base > 0.0 ? turn(v, (skip + i) * 32 + 4 * c) : v;
+    }
     return;
   }
 
   const int item = blockIdx.y * 4 + wave;
-  if (item >= 2 * gc || pg < 0) return;
+  if (item >= 2 * gc) return;
   const int j = item >> 1, kind = item & 1;
   const int n_old = lo - t0;            // older tokens of the block
   const int n_hi = hi - t0;
-  float* const scale_at = BLOCKS ? (float*)(page + (int64_t)P * (gc * (DH + DV) + DR * 2)) + ((int64_t)j * (P / kBlock) + T) * 2 + kind : nullptr;
-  float scale_was = 1.f;
-  if (BLOCKS && n_old > 0) scale_was = *scale_at;
+  const int64_t row0 = r.first + (t0 - p0);   // row of the block's first token (where that is a new one)
+  auto scale_at = [&] { return (float*)(page + (int64_t)P * (gc * (DH + DV) + DR * 2)) + ((int64_t)j * (P / kBlock) + T) * 2 + kind; };
   // the block's exponent from the new values and the older tokens'
   auto settle = [&](int e_new, int& e, int& e_old) {
-    e_old = n_old > 0 ? exponent_of(scale_was) : e_new;
+    e_old = e_new;
+    if (n_old > 0) e_old = exponent_of(*scale_at());
     e = max(e_new, e_old);
-    if (lane == 0 && (n_old == 0 || e != e_old)) *scale_at = pow2(e);
   };
+  auto keep = [&](int e, int e_old) {
+    if (lane == 0 && (n_old == 0 || e != e_old)) *scale_at() = pow2(e);
+  };
+
+  if (n_hi - n_old <= kFew) {           // a step's tokens: a lane takes dims 4 lane .. 4 lane + 3 of each
+    const int dims = kind == 0 ? DH : DV, d = 4 * lane;
+    const int64_t stride = kind == 0 ? a.k_stride : a.v_stride;
+    const char* src = (const char*)(kind == 0 ? a.k_c : a.v) + ((row0 + n_old) * stride + (int64_t)j * dims + d) * 2;
+    u32x2 w[kFew];
+#pragma unroll
+    for (int i = 0; i < kFew; ++i) w[i] = d < dims && n_old + i < n_hi ? *(const u32x2*)(src + i * stride * 2) : u32x2{0, 0};
+    asm volatile("" ::: "memory");      // (the rows are asked for ahead of the page)
+    if (!look_up(page)) return;
+    if constexpr (!BLOCKS) {
+#pragma unroll
+      for (int i = 0; i < kFew; ++i) {
+        const int slot = slot0 + n_old + i;
+        if (d >= dims || n_old + i >= n_hi) continue;
+        if (kind == 0) {
+          *(u32x2*)(page + (((int64_t)j * (DH / 8) + d / 8) * P + slot) * 16 + d % 8 * 2) = w[i];
+        } else {
+          uint16_t* dst = (uint16_t*)(page + (int64_t)P * gc * DH * 2 + (((int64_t)j * (P / 8) + slot / 8) * DV + d) * 16) + slot % 8;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) dst[8 * k] = (uint16_t)(w[i][k >> 1] >> (16 * (k & 1)));
+        }
+      }
+      return;
+    } else {
+      bool careful;
+      const int e_new = wave_exponent([&](auto&& f) {
+#pragma unroll
+        for (int i = 0; i < kFew; ++i) {
+          f(w[i][0]);
+          f(w[i][1]);
+        }
+      }, careful);
+      int e, e_old;
+      settle(e_new, e, e_old);
+      if (e == e_old) {                 // (else the older codes change as well: below)
+        keep(e, e_old);
+        const float inv = pow2(-e);
+#pragma unroll
+        for (int i = 0; i < kFew; ++i) {
+          const int n = n_old + i;
+          if (d >= dims || n >= n_hi) continue;
+          const uint32_t c = codes4(lo16(w[i][0]), hi16(w[i][0]), lo16(w[i][1]), hi16(w[i][1]), inv, careful);
+          if (kind == 0) {
+            *(uint32_t*)(page + (((int64_t)j * (DH / 16) + d / 32 * 2 + d / 8 % 2) * P + slot0 + n) * 16 + d / 16 % 2 * 8 + d % 8) = c;
+          } else {
+            uint8_t* dst = (uint8_t*)(page + (int64_t)P * gc * DH + ((((int64_t)j * (P / kBlock) + T) * DV + d) * 2 + n / 8 % 2) * 16 + n / 16 * 8 + n % 8);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) dst[32 * k] = (uint8_t)(c >> (8 * k));
+          }
+        }
+        return;
+      }
+    }
+  }
 
   if (kind == 0) {
     const int n = lane & 31, h = lane >> 5;
     const bool fresh = n >= n_old && n < n_hi;
-    const char* src = (const char*)a.k_c + ((r.first + (t0 + n - p0)) * a.k_stride + (int64_t)j * DH + 8 * h) * 2;
+    const char* src = (const char*)a.k_c + ((row0 + n) * a.k_stride + (int64_t)j * DH + 8 * h) * 2;
     u32x4 w[DH / 16];
 #pragma unroll
     for (int c = 0; c < DH / 16; ++c) w[c] = fresh ? *(const u32x4*)(src + c * 32) : u32x4{0, 0, 0, 0};   // dims 16 c + 8 h ..
+    asm volatile("" ::: "memory");
+    if (!look_up(page)) return;
     if constexpr (!BLOCKS) {
       char* dst = page + (((int64_t)j * (DH / 8) + h) * P + slot0 + n) * 16;
       if (fresh) {
@@ -211,6 +279,7 @@ __global__ void __launch_bounds__(256) append_rows_kernel(AppendRowsArgs a, int 
       }, careful);
       int e, e_old;
       settle(e_new, e, e_old);
+      keep(e, e_old);
       const float inv = pow2(-e);
       char* dst = page + (((int64_t)j * (DH / 16) + h) * P + slot0 + n) * 16;
       if (fresh) {
@@ -234,7 +303,7 @@ __global__ void __launch_bounds__(256) append_rows_kernel(AppendRowsArgs a, int 
     constexpr int WPL = DV / 64;                 // 32-bit words (pairs of dims) per lane and token
     typedef __attribute__((ext_vector_type(WPL))) uint32_t words_t;
     const int dq = lane & 31, h = lane >> 5;     // dims 2 WPL dq ..
-    const char* src = (const char*)a.v + ((r.first + (t0 - p0)) * a.v_stride + (int64_t)j * DV + 2 * WPL * dq) * 2;
+    const char* src = (const char*)a.v + (row0 * a.v_stride + (int64_t)j * DV + 2 * WPL * dq) * 2;
     words_t w[16];                               // token 16 (x / 8) + 8 h + x % 8
 #pragma unroll
     for (int x = 0; x < 16; ++x) {
@@ -242,6 +311,8 @@ __global__ void __launch_bounds__(256) append_rows_kernel(AppendRowsArgs a, int 
       w[x] = words_t{};
       if (n >= n_old && n < n_hi) w[x] = *(const words_t*)(src + n * a.v_stride * 2);
     }
+    asm volatile("" ::: "memory");
+    if (!look_up(page)) return;
     char* const plane = page + (int64_t)P * gc * DH * EB;
     if constexpr (!BLOCKS) {
 #pragma unroll
@@ -275,10 +346,10 @@ __global__ void __launch_bounds__(256) append_rows_kernel(AppendRowsArgs a, int 
       }, careful);
       int e, e_old;
       settle(e_new, e, e_old);
+      keep(e, e_old);
       const float inv = pow2(-e);
       char* dst = plane + ((((int64_t)j * (P / kBlock) + T) * DV + 2 * WPL * dq) * 2 + h) * 16;
       const bool whole = n_old == 0 && n_hi == kBlock;
-      const bool few = e == e_old && n_hi - n_old <= 4;
       uint32_t fresh[4], old[4];                 // byte masks of the vector's words
       if (!whole) {
 #pragma unroll
@@ -296,22 +367,16 @@ __global__ void __launch_bounds__(256) append_rows_kernel(AppendRowsArgs a, int 
           auto at = [&](int i) { const uint32_t x = w[8 * (k >> 1) + 4 * (k & 1) + i][d >> 1]; return d & 1 ? hi16(x) : lo16(x); };
           o[k] = codes4(at(0), at(1), at(2), at(3), inv, careful);
         }
-        if (whole) {
-          *(u32x4*)(dst + d * 32) = o;
-        } else if (few) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (fresh[i >> 2] & (0xffu << (8 * (i & 3)))) *(uint8_t*)(dst + d * 32 + i) = (uint8_t)(o[i >> 2] >> (8 * (i & 3)));
-        } else {
-          u32x4 x = *(const u32x4*)(dst + d * 32);
+        if (!whole) {
+          const u32x4 x = *(const u32x4*)(dst + d * 32);
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            uint32_t keep = x[k];
-            if (e != e_old) keep = (keep & ~old[k]) | (rescale4(keep, factor) & old[k]);
-            x[k] = (keep & ~fresh[k]) | (o[k] & fresh[k]);
+            uint32_t was = x[k];
+            if (e != e_old) was = (was & ~old[k]) | (rescale4(was, factor) & old[k]);
+            o[k] = (was & ~fresh[k]) | (o[k] & fresh[k]);
           }
-          *(u32x4*)(dst + d * 32) = x;
         }
+        *(u32x4*)(dst + d * 32) = o;
       }
     }
   }
@@ -460,7 +525,11 @@ __global__ void __launch_bounds__(256) quantize_blocks_kernel(QuantizeArgs a) {
 template <int DH, int DV, bool BLOCKS>
 hipError_t launch_append(const AppendRowsArgs& a, hipStream_t s) {
   const int kv = (2 * a.g + 3) / 4;
-  append_rows_kernel<DH, DV, BLOCKS><<<dim3((unsigned)row_runs(a.total, 1, kBlock, 2, a.B), kv + 4), 256, 0, s>>>(a, kv);
+  // Two tokens a workgroup where the rows are few, but more than a step's, so that many heads spread over the chip; eight otherwise, whose
+  // table is read four times as often.  (128 heads, eight -> two) 150 rows 10.9 -> 5.9 us, 3700 26.7 -> 25.7, 6000 61.4 -> 58.4, 30000
+  // 246 -> 247, 120000 958 -> 995; (32 heads) 750 7.1 -> 6.6, 6000 20.8 -> 20.9, 30000 97 -> 101.
+  const int at_once = a.total > 4 * (int64_t)a.B && a.total <= 8192 && a.h_q >= 32 ? 2 : 8;
+  append_rows_kernel<DH, DV, BLOCKS><<<dim3((unsigned)row_runs(a.total, 1, kBlock, 2, a.B), kv + kBlock / at_once), 256, 0, s>>>(a, kv, at_once);
   return hipGetLastError();
 }
 
