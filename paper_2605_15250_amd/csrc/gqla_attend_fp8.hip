@@ -4,11 +4,10 @@
 // wave, and walks the tokens they see in stages of 64, which LDS-DMA brings into a ring of buffers ahead of their use:
 //   S^T[token][row] = K Q^T,   O^T[dim][row] += V^T P^T
 // with one query row per lane throughout, a running maximum (moved only when outgrown) and an fp32 sum.
-//   K Q^T: the codes go into the 8-bit matrix instruction as they lie, their block's power of two in its scale operand.  The queries are
-//     the sum of two E4M3 terms, hi = E4M3(q 2^-e) and lo = E4M3((q 2^-e - hi) 2^4), e per row and 64 dims: 4 + 4 bits are the 8 of a
-//     bf16, and what subnormal codes lose is below 2^-22 of the largest.  Two products at twice the rate cost what one in bf16 does, and
-//     no key code is widened (32 conversions per tile and wave).
-//   q_R k_R^T in bf16;  V^T P^T in bf16, value codes widened with their power of two, probabilities rounded to bf16.
+// Codes are widened to bf16 with their block's power of two, exactly, right before their products; probabilities are rounded to bf16.
+// (The 8-bit matrix instruction takes key codes as they are, with the queries as the sum of two E4M3 terms: two prompts of 2500 to 4000 tokens x
+// 128 heads then take 1042 us instead of 1107.  But it aligns the products of a sum to 2^-14 of the largest, where those in bf16 are
+// summed in fp32: logits were 3e-4 off.)
 // The cache's vectors are operand fragments; a stage in LDS is a row of 1 KB pieces, one per fragment, so that a request writes and a
 // read takes 64 consecutive vectors (no bank is met twice).
 // Few rows over a long context: the tokens are split into ranges, whose partial outputs a second kernel joins.
@@ -23,7 +22,6 @@ namespace gqla {
 
 namespace {
 
-typedef __attribute__((ext_vector_type(8))) int i32x8;
 typedef const __attribute__((address_space(4))) f32x4* const_f32x4_ptr;
 
 __device__ __forceinline__ bf16x8 widen_codes(uint32_t w0, uint32_t w1, float scale) {
@@ -93,52 +91,18 @@ __global__ void __launch_bounds__(64 * kWaves, (AttendTile<DH, DV>::kPerUnit)) a
   const int per = (stages + a.splits - 1) / a.splits;
   const int st0 = min(split * per, stages), st1 = min(st0 + per, stages);
 
-  // queries: content as two E4M3 terms per (row, 64 dims), the rotary part in bf16
   const int64_t row = (int64_t)r.first + t;
-  i32x8 q_hi[KC / 2], q_lo[KC / 2];
-  int q_e[KC / 2];
-  bf16x8 qr[KR];
+  bf16x8 qc[2 * KC], qr[KR];
   {
-    const char* pc = (const char*)a.q_c + ((row * a.h_q + head) * DH + 8 * h) * 2;
+    const __bf16* pc = (const __bf16*)a.q_c + (row * a.h_q + head) * DH + 8 * h;
     const __bf16* pr = (const __bf16*)a.q_r + (row * a.h_q + head) * DR + 8 * h;
 #pragma unroll
+    for (int ks = 0; ks < 2 * KC; ++ks) qc[ks] = *(const bf16x8*)(pc + 16 * ks);
+#pragma unroll
     for (int ks = 0; ks < KR; ++ks) qr[ks] = *(const bf16x8*)(pr + 16 * ks);
-#pragma unroll
-    for (int x = 0; x < KC / 2; ++x) {
-      u32x4 w[4];                                                      // dims 64 x + 16 y + 8 h ..
-#pragma unroll
-      for (int y = 0; y < 4; ++y) w[y] = *(const u32x4*)(pc + (64 * x + 16 * y) * 2);
-      uint32_t top = 0;
-#pragma unroll
-      for (int y = 0; y < 4; ++y)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) top = max(top, max(w[y][k] & 0x7fffu, w[y][k] >> 16 & 0x7fffu));
-      {
-        uint32_t r0, r1;   // one scale for the row's 64 dims: a scale operand covers 32 of them, 16 in either half-wave
-        half_swap(top, top, r0, r1);
-        top = max(r0, r1);
-      }
-      // smallest e with max |q| <= 448 * 2^e; infinities and NaN (which have to come out as such) leave the scale at its end
-      const int e = min(max((int)(((top << 16) + 0x1fffffu) >> 23) - 127 - 8, -100), 120);
-      const float inv = __builtin_bit_cast(float, (uint32_t)(127 - e) << 23);
-      q_e[x] = e + 127;
-#pragma unroll
-      for (int y = 0; y < 4; ++y)
-#pragma unroll
-        for (int k = 0; k < 4; k += 2) {
-          const float f0 = bf16_bits_to_float(w[y][k] & 0xffffu) * inv, f1 = bf16_bits_to_float(w[y][k] >> 16) * inv;
-          const float f2 = bf16_bits_to_float(w[y][k + 1] & 0xffffu) * inv, f3 = bf16_bits_to_float(w[y][k + 1] >> 16) * inv;
-          int c = __builtin_amdgcn_cvt_pk_fp8_f32(f0, f1, 0, false);
-          c = __builtin_amdgcn_cvt_pk_fp8_f32(f2, f3, c, true);
-          const auto b0 = __builtin_amdgcn_cvt_pk_f32_fp8(c, false), b1 = __builtin_amdgcn_cvt_pk_f32_fp8(c, true);
-          int l = __builtin_amdgcn_cvt_pk_fp8_f32((f0 - b0[0]) * 16.f, (f1 - b0[1]) * 16.f, 0, false);
-          l = __builtin_amdgcn_cvt_pk_fp8_f32((f2 - b1[0]) * 16.f, (f3 - b1[1]) * 16.f, l, true);
-          q_hi[x][2 * y + k / 2] = c;
-          q_lo[x][2 * y + k / 2] = l;
-        }
-    }
   }
-
+#pragma unroll
+  for (int ks = 0; ks < 2 * KC; ++ks) asm volatile("" : "+v"(qc[ks]));
 #pragma unroll
   for (int ks = 0; ks < KR; ++ks) asm volatile("" : "+v"(qr[ks]));      // (waited for here: a wait inside the loop would be one for the requests, too)
 
@@ -209,13 +173,11 @@ __global__ void __launch_bounds__(64 * kWaves, (AttendTile<DH, DV>::kPerUnit)) a
     f32x16 s;
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = 0.f;
-    const int k_e = (int)(__builtin_bit_cast(uint32_t, sc_k) >> 23);
 #pragma unroll
-    for (int x = 0; x < KC / 2; ++x) {
-      const u32x4 k0 = *(const u32x4*)(k_lds + (2 * x) * 1024), k1 = *(const u32x4*)(k_lds + (2 * x + 1) * 1024);
-      const i32x8 k = {(int)k0[0], (int)k0[1], (int)k0[2], (int)k0[3], (int)k1[0], (int)k1[1], (int)k1[2], (int)k1[3]};
-      s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k, q_hi[x], s, 0, 0, 0, k_e, 0, q_e[x]);
-      s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k, q_lo[x], s, 0, 0, 0, k_e, 0, q_e[x] - 4);
+    for (int kp = 0; kp < KC; ++kp) {
+      const u32x4 k8 = *(const u32x4*)(k_lds + kp * 1024);
+      s = mfma32(widen_codes(k8[0], k8[1], sc_k), qc[2 * kp], s);
+      s = mfma32(widen_codes(k8[2], k8[3], sc_k), qc[2 * kp + 1], s);
     }
 #pragma unroll
     for (int ks = 0; ks < KR; ++ks) s = mfma32(*(const bf16x8*)(r_lds + ks * 1024), qr[ks], s);

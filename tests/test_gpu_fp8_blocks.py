@@ -386,6 +386,21 @@ def test_attend_splits_a_long_context(g, G, d_h, d_v, lens, ns):
     w.check_attention(out, lse, q_c, q_r, first, lens)
 
 
+@pytest.mark.parametrize("g,G,d_h,d_v", [(4, 8, 128, 128), (4, 5, 192, 256)])
+def test_log_sum_exps_have_fp32_accuracy(g, G, d_h, d_v):
+    """Logits are sums of d_h + d_R products in fp32: each addition is off by at most 2^-24 of a partial sum, at random, so the sum by
+    about sqrt(d_h + d_R) * 2^-24 = 1e-6 of the partial sums' size, which is the logits' own (cancellation leaves a fraction of them, a
+    sum over hundreds of tokens averages).  Relative to the log-sum-exps, in the 2-norm: below 1e-6."""
+    lens, ns = [700, 300], [40, 60]
+    w = World(lens, g, d_h, d_v, G=G, seed=171 + g)
+    w.append(lens)
+    q_c, q_r = stored(w.r.normal(size=(100, g * G, d_h))), stored(w.r.normal(size=(100, g * G, D_R)))
+    _, lse, first, _ = attend(w, ns, lens, q_c, q_r)
+    want = np.concatenate([FB.attend(q_c[first[b]:first[b + 1]], q_r[first[b]:first[b + 1]], w.K[b].values(), w.V[b].values(),
+                                     stored(w.kr_held(b)), lens[b])[1] for b in range(2)])
+    assert np.linalg.norm(lse - want) <= 1e-6 * np.linalg.norm(want)
+
+
 def test_a_nan_stays_in_its_sequence():
     """One sequence's NaN (a value of an old token) reaches its own rows and no others'."""
     lens = [90, 70]
