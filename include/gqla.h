@@ -372,7 +372,7 @@ typedef struct {
  * Block scales: a block that begins inside the new rows takes its exponent from them.  A block that holds older tokens keeps the
  * larger of its own exponent and the one that the new rows need; where it grows, the older codes are rounded to the new
  * scale (exact but for codes that fall below E4M3's normal range).  Appending the same rows again changes nothing.
- * Errors: GQLA_ERR_SHAPE for another group count, rope_base, total < 0, total > 2^30, batch > 2^24, d_r odd or above 512; GQLA_ERR_NULL for q_r without
+ * Errors: GQLA_ERR_SHAPE for another group count, rope_base, total < 0, total > 2^23, batch > 2^20, d_r odd or above 512; GQLA_ERR_NULL for q_r without
  * q_rot or the reverse; others as for gqla_append_latent.  Both calls only enqueue one kernel on `stream`. */
 gqla_status gqla_append_expanded(const gqla_shape* shape, const gqla_new_rows* rows, float rope_base, const gqla_cache* expanded,
                                  void* stream);
@@ -387,8 +387,10 @@ gqla_status gqla_append_expanded_fp8_blocks(const gqla_shape* shape, const gqla_
  * that no sequence owns are not touched.  A NaN among the values of a tile of 32 tokens reaches every row that has a token of the tile in sight.
  * ws: device scratch of at least gqla_attend_gqa_workspace_bytes(shape, first, total, expanded_blocks) bytes, 16-byte aligned (fp32
  * partial outputs over ranges of a long context, where there are few rows; may be NULL when that is 0).  It depends on the sizes
- * only, max_pages * page_size standing for the longest context; its content is the call's own.
- * Errors: GQLA_ERR_WORKSPACE when ws is missing or too small, GQLA_ERR_SHAPE when total * h_q / g or the launch exceeds 2^31; others as above. */
+ * only, max_pages * page_size standing for the longest context, and holds nothing between calls; calls whose kernels can overlap
+ * (other streams, graphs replayed side by side) need one each.
+ * Errors: GQLA_ERR_WORKSPACE when ws is missing or too small; GQLA_ERR_SHAPE when total * h_q / g exceeds 2^31, the launch 2^24 workgroups
+ * (one per 128 query rows of a sequence and group, and per range of the context) or a page 2^31 bytes; others as above. */
 gqla_status gqla_attend_gqa_fp8_blocks(const gqla_shape* shape, const int32_t* first, int32_t total, const void* q_c, const void* q_r,
                                        const gqla_cache* expanded_blocks, void* out, float* lse, void* ws, size_t ws_bytes,
                                        void* stream);

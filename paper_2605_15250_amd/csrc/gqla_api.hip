@@ -879,7 +879,7 @@ gqla_status check_packed(const gqla_shape* shape, const int32_t* first, int32_t 
   if (st != GQLA_OK) return st;
   if (!expanded || !expanded->pool || !expanded->seq_lens) return GQLA_ERR_NULL;
   if ((reinterpret_cast<uintptr_t>(first) & 3u) || (reinterpret_cast<uintptr_t>(expanded->seq_lens) & 3u)) return GQLA_ERR_ALIGN;
-  if (total < 0 || total > (1 << 30) || shape->batch > (1 << 24) || expanded->groups != shape->g) return GQLA_ERR_SHAPE;
+  if (total < 0 || total > (1 << 23) || shape->batch > (1 << 20) || expanded->groups != shape->g) return GQLA_ERR_SHAPE;   // a launch has 2^32 threads at most
   if (!first && total != (int64_t)shape->batch * shape->s_q) return GQLA_ERR_SHAPE;
   st = check_page_size(shape, expanded->page_size);
   return st == GQLA_OK ? check_cache(shape, expanded, expanded->page_size, 0) : st;
@@ -969,10 +969,8 @@ gqla_status gqla_attend_gqa_fp8_blocks(const gqla_shape* shape, const int32_t* f
   // offsets inside a page are 32-bit
   if (gqla_expanded_fp8_blocks_page_bytes(shape->g, shape->d_h, value_dim(shape), shape->d_r, expanded_blocks->page_size) > INT32_MAX)
     return GQLA_ERR_SHAPE;
-  // (row runs, 32 rows each at the least, of all groups and splits are workgroups of one launch)
-  if ((int64_t)total * a.G > INT32_MAX || ((int64_t)total * a.G / 32 + shape->batch) * shape->g > INT32_MAX / a.splits ||
-      (int64_t)total * shape->h_q > INT32_MAX)
-    return GQLA_ERR_SHAPE;
+  // rows in 32 bits, and 2^24 workgroups of 256 threads at most: tiles of 128 rows of all sequences and groups, times the ranges
+  if ((int64_t)total * a.G > INT32_MAX || ((int64_t)total * a.G / 128 + shape->batch + 8) * shape->g > (1 << 24) / a.splits) return GQLA_ERR_SHAPE;
   if (a.splits > 1 && (!ws || ws_bytes < attend_bytes(shape, total, a.splits))) return GQLA_ERR_WORKSPACE;
   a.q_c = q_c;
   a.q_r = q_r;

@@ -450,7 +450,8 @@ int attend_splits(int64_t total, int64_t batch, int h_q, int g, int d_h, int64_t
   const int64_t stages = (max_tokens + kStage - 1) / kStage;
   int best = 1;
   double best_us = 0;
-  for (int s = 1; s <= 64 && s <= stages; ++s) {
+  const int most = total * h_q > (1 << 24) ? 1 : 64;                   // (the merge has a workgroup per row at the most)
+  for (int s = 1; s <= most && s <= stages; ++s) {
     const double n = (double)tiles * s, length = (double)((stages + s - 1) / s + 2);
     const int k = n >= 256.0 * per_unit ? per_unit : std::max(1, (int)std::ceil(n / 256.0));
     double us = length * stage[k - 1] * (n > 256.0 * per_unit ? n / 256.0 + 0.5 * per_unit : k);

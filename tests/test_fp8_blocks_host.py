@@ -92,7 +92,7 @@ def test_append_refusals(fn):
     for odd in ({"k_c": A + 2}, {"v": A + 8}, {"k_r": A + 4}, {"q_r": A + 8, "q_rot": A}, {"q_r": A, "q_rot": A + 8}, {"first": A + 2},
                 {"k_stride": 1028}, {"v_stride": 1025}, {"kr_stride": 66}):
         _refused(B.GQLA_ERR_ALIGN, call, rows=_rows(**odd))
-    for wrong in ({"total": -1}, {"total": (1 << 30) + 1}, {"k_stride": 1016}, {"v_stride": 8}, {"kr_stride": 56}, {"k_stride": -1024},
+    for wrong in ({"total": -1}, {"total": (1 << 23) + 1}, {"k_stride": 1016}, {"v_stride": 8}, {"kr_stride": 56}, {"k_stride": -1024},
                   {"first": None, "total": 3}):
         _refused(B.GQLA_ERR_SHAPE, call, rows=_rows(**wrong))
     for base in (1.0, -2.0, 0.5, float("nan"), float("inf")):
@@ -152,6 +152,9 @@ def test_attend_refusals_and_workspace():
     _refused(B.GQLA_ERR_SHAPE, call, total=-1)
     _refused(B.GQLA_ERR_SHAPE, call, first=None, total=7)
     _refused(B.GQLA_ERR_SHAPE, call, shape=_shape(h_q=1 << 14, g=8), total=1 << 20)      # 2^31 query rows of a group
+    _refused(B.GQLA_ERR_SHAPE, call, shape=_shape(h_q=1 << 12, g=1 << 11), cache=_cache(groups=1 << 11), total=1 << 20)   # 2^25 workgroups
+    _refused(B.GQLA_ERR_SHAPE, call, shape=_shape(batch=(1 << 20) + 1), cache=_cache(num_pages=1 << 23))
+    _refused(B.GQLA_ERR_SHAPE, call, shape=_shape(h_q=1 << 16, g=1 << 14), cache=_cache(groups=1 << 14, page=1024), total=8)   # a page of 2^32 bytes
     _refused(B.GQLA_ERR_SHAPE, call, cache=_cache(groups=7))
     _refused(B.GQLA_ERR_PAGE, call, cache=_cache(page=96))
     call(total=0)

@@ -215,7 +215,7 @@ def test_append_more_than_64_sequences_and_uniform_steps():
 
 def test_append_edges():
     """Infinities, NaN, zeros, values beyond the scales; no rotation and no queries; the same rows again."""
-    w = World([90, 64], 2, seed=41)
+    w = World([90, 64 + 3], 2, seed=41)
     k, v, kr = w.draw_rows(77)
     k[3, 0, 5], k[9, 1, 2], v[11, 0, 7], v[12, 1, 0] = np.inf, np.nan, -np.inf, np.nan
     k[40:], v[40:45] = 0.0, stored(3.2e38)
@@ -224,6 +224,13 @@ def test_append_edges():
     rows = w.draw_rows(3)
     w.append([3, 0], rows=rows)
     w.check_pool()
+    for bad in (np.nan, np.inf, -np.inf):                 # alone in a step's row, K and V
+        k1, v1, kr1 = w.draw_rows(2)
+        k1[0, 0, 3], v1[0, 1, 100], v1[1, 0, 127] = bad, bad, bad
+        w.append([1, 1], rows=(k1, v1, kr1))
+        w.check_pool()
+    rows = w.draw_rows(3)
+    w.append([3, 0], rows=rows)
     before = w.pool.clone()
     first = torch.tensor([0, 3, 3], dtype=torch.int32, device="cuda")
     new = B.make_new_rows(bf16(rows[0].reshape(3, -1)).cuda(), bf16(rows[1].reshape(3, -1)).cuda(), bf16(rows[2]).cuda(), first=first, total=3)
@@ -411,6 +418,35 @@ def test_a_nan_stays_in_its_sequence():
     q_c, q_r = stored(w.r.normal(size=(20, 8, 128))), stored(w.r.normal(size=(20, 8, D_R)))
     out, lse, _, _ = attend(w, [10, 10], lens, q_c, q_r)
     assert np.all(np.isnan(out[:10, :4, 0])) and np.all(np.isfinite(out[:10, :, 1:])) and np.all(np.isfinite(out[10:])) and np.all(np.isfinite(lse))
+
+
+def test_pages_beyond_4_gib():
+    """Pages at the end of a pool of 5.2 GB: appends, conversion, both attention calls."""
+    lens = [130, 70]
+    w = World(lens, 8, G=2, seed=151, s_q=1)
+    pages = 38000
+    w.table = np.where(w.table >= 0, w.table + pages - w.pages, -1).astype(np.int32)
+    w.d_table = torch.from_numpy(w.table).cuda()
+    w.pool = torch.zeros((pages, w.bytes), dtype=torch.uint8, device="cuda")
+    assert int(w.table[w.table >= 0].min()) * w.bytes > 1 << 32
+    shift, w.pages = pages - w.pages, pages
+    w.append(lens)
+    # the few pages that hold something, as a pool of their own
+    small = World(lens, 8, G=2, seed=151, s_q=1)
+    small.K, small.V, small.kr = w.K, w.V, w.kr
+    small.pool = w.pool[shift:].clone()
+    assert not bool(w.pool[:shift].any())
+    q_c, q_r = stored(w.r.normal(size=(30, 16, 128))), stored(w.r.normal(size=(30, 16, D_R)))
+    out, lse, first, _ = attend(w, [20, 10], lens, q_c, q_r)
+    small.check_attention(out, lse, q_c, q_r, first, lens)
+    plan = B.gqla_plan_create(w.shape, w.lens(), w.P, NUM_CUS, B.GQLA_PATH_GQA)
+    ws = torch.empty(B.gqla_plan_workspace_bytes(plan), dtype=torch.uint8, device="cuda")
+    B.gqla_plan_upload(plan, ws)
+    out, lse = torch.empty((2, 16, 128), dtype=torch.bfloat16, device="cuda"), torch.empty((2, 16), device="cuda")
+    B.gqla_decode_gqa_fp8_blocks(w.shape, plan, bf16(q_c[:2]).cuda(), bf16(q_r[:2]).cuda(), w.cache(), out, lse, ws)
+    torch.cuda.synchronize()
+    B.gqla_plan_destroy(plan)
+    small.check_attention(out.float().cpu().numpy(), lse.cpu().numpy(), q_c[:2], q_r[:2], [0, 1, 2], lens)
 
 
 # ---- together -----------------------------------------------------------------------------------------------------------
