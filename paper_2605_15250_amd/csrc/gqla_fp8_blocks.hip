@@ -98,9 +98,9 @@ __device__ __forceinline__ uint32_t token_bytes(int w, int h, int a, int b) {
 }
 
 // ---- rows of new tokens ----------------------------------------------------------------------------------------------
-// One wave per (sequence, block of 32 positions, group, K or V): it alone owns what it writes, its scale included, so there is
+// One wave per (sequence, block of 32 positions, group, K or V; 16-bit values of 256 dims are two waves' work): it alone owns what it writes, its scale included, so there is
 // nothing to synchronise.  K: a lane takes one token and every second run of 8 dims, which are output vectors as they are.  V: a lane takes
-// 4 dims (8 with a value dim of 256) and the 16 tokens of an output vector, so that a load covers whole rows of two tokens and the turn from
+// 4 dims (8 of 256 as codes) and the 16 tokens of an output vector, so that a load covers whole rows of two tokens and the turn from
 // token-major to dim-major happens in registers; vectors that others share are stored element by element or, as codes, read, changed and
 // written back.  At most four new tokens (a step): a lane takes four dims of each, and codes are stored byte by byte, with no read of
 // what is there; only where the block's older codes need a larger exponent is this the long way again.
@@ -182,9 +182,11 @@ __global__ void __launch_bounds__(256) append_rows_kernel(AppendRowsArgs a, int 
     return;
   }
 
+  // K, then V: codes in one piece (the scale is the whole block's), 16 bits in pieces of 128 dims
+  constexpr int VD = BLOCKS ? DV : 128, UNITS = 1 + DV / VD;
   const int item = blockIdx.y * 4 + wave;
-  if (item >= 2 * gc) return;
-  const int j = item >> 1, kind = item & 1;
+  if (item >= UNITS * gc) return;
+  const int j = item / UNITS, kind = item % UNITS > 0, v0 = max(item % UNITS - 1, 0) * VD;
   const int n_old = lo - t0;            // older tokens of the block
   const int n_hi = hi - t0;
   const int64_t row0 = r.first + (t0 - p0);   // row of the block's first token (where that is a new one)
@@ -200,9 +202,9 @@ __global__ void __launch_bounds__(256) append_rows_kernel(AppendRowsArgs a, int 
   };
 
   if (n_hi - n_old <= kFew) {           // a step's tokens: a lane takes dims 4 lane .. 4 lane + 3 of each
-    const int dims = kind == 0 ? DH : DV, d = 4 * lane;
+    const int dims = kind == 0 ? DH : v0 + VD, d = v0 + 4 * lane;
     const int64_t stride = kind == 0 ? a.k_stride : a.v_stride;
-    const char* src = (const char*)(kind == 0 ? a.k_c : a.v) + ((row0 + n_old) * stride + (int64_t)j * dims + d) * 2;
+    const char* src = (const char*)(kind == 0 ? a.k_c : a.v) + ((row0 + n_old) * stride + (int64_t)j * (kind == 0 ? DH : DV) + d) * 2;
     u32x2 w[kFew];
 #pragma unroll
     for (int i = 0; i < kFew; ++i) w[i] = d < dims && n_old + i < n_hi ? *(const u32x2*)(src + i * stride * 2) : u32x2{0, 0};
@@ -300,10 +302,10 @@ __global__ void __launch_bounds__(256) append_rows_kernel(AppendRowsArgs a, int 
       }
     }
   } else {
-    constexpr int WPL = DV / 64;                 // 32-bit words (pairs of dims) per lane and token
+    constexpr int WPL = VD / 64;                 // 32-bit words (pairs of dims) per lane and token
     typedef __attribute__((ext_vector_type(WPL))) uint32_t words_t;
-    const int dq = lane & 31, h = lane >> 5;     // dims 2 WPL dq ..
-    const char* src = (const char*)a.v + (row0 * a.v_stride + (int64_t)j * DV + 2 * WPL * dq) * 2;
+    const int dq = lane & 31, h = lane >> 5, d0 = v0 + 2 * WPL * dq;   // dims d0 ..
+    const char* src = (const char*)a.v + (row0 * a.v_stride + (int64_t)j * DV + d0) * 2;
     words_t w[16];                               // token 16 (x / 8) + 8 h + x % 8
 #pragma unroll
     for (int x = 0; x < 16; ++x) {
@@ -319,7 +321,7 @@ __global__ void __launch_bounds__(256) append_rows_kernel(AppendRowsArgs a, int 
       for (int u = 0; u < 2; ++u) {
         const int n0 = 16 * u + 8 * h;           // tokens n0 .. n0 + 7 of this lane's vectors
         if (n0 + 8 <= n_old || n0 >= n_hi) continue;
-        char* dst = plane + (((int64_t)j * (P / 8) + slot0 / 8 + 2 * u + h) * DV + 2 * WPL * dq) * 16;
+        char* dst = plane + (((int64_t)j * (P / 8) + slot0 / 8 + 2 * u + h) * DV + d0) * 16;
         const bool whole = n0 >= n_old && n0 + 8 <= n_hi;
 #pragma unroll
         for (int d = 0; d < 2 * WPL; ++d) {
@@ -348,7 +350,7 @@ __global__ void __launch_bounds__(256) append_rows_kernel(AppendRowsArgs a, int 
       settle(e_new, e, e_old);
       keep(e, e_old);
       const float inv = pow2(-e);
-      char* dst = plane + ((((int64_t)j * (P / kBlock) + T) * DV + 2 * WPL * dq) * 2 + h) * 16;
+      char* dst = plane + ((((int64_t)j * (P / kBlock) + T) * DV + d0) * 2 + h) * 16;
       const bool whole = n_old == 0 && n_hi == kBlock;
       uint32_t fresh[4], old[4];                 // byte masks of the vector's words
       if (!whole) {
@@ -524,7 +526,7 @@ __global__ void __launch_bounds__(256) quantize_blocks_kernel(QuantizeArgs a) {
 
 template <int DH, int DV, bool BLOCKS>
 hipError_t launch_append(const AppendRowsArgs& a, hipStream_t s) {
-  const int kv = (2 * a.g + 3) / 4;
+  const int kv = ((BLOCKS ? 2 : 1 + DV / 128) * a.g + 3) / 4;
   // Two tokens a workgroup where the rows are few, but more than a step's, so that many heads spread over the chip; eight otherwise, whose
   // table is read four times as often.  (128 heads, eight -> two) 150 rows 10.9 -> 5.9 us, 3700 26.7 -> 25.7, 6000 61.4 -> 58.4, 30000
   // 246 -> 247, 120000 958 -> 995; (32 heads) 750 7.1 -> 6.6, 6000 20.8 -> 20.9, 30000 97 -> 101.
