@@ -931,8 +931,8 @@ gqla_status append_impl(const gqla_shape* shape, const gqla_new_rows* rows, floa
   return e == hipSuccess ? GQLA_OK : GQLA_ERR_DEVICE;
 }
 
-int attend_splits_of(const gqla_shape* shape, int32_t total, const gqla_cache* expanded) {
-  return attend_splits(total, shape->batch, shape->h_q, shape->g, shape->d_h, (int64_t)expanded->max_pages * expanded->page_size);
+void attend_shape_of(const gqla_shape* shape, int32_t total, const gqla_cache* expanded, int32_t* splits, int32_t* tile_shift) {
+  attend_shape(total, shape->batch, shape->h_q, shape->g, shape->d_h, (int64_t)expanded->max_pages * expanded->page_size, splits, tile_shift);
 }
 size_t attend_bytes(const gqla_shape* shape, int32_t total, int splits) {
   return splits > 1 ? (size_t)splits * total * shape->h_q * (value_dim(shape) + 1) * sizeof(float) : 0;
@@ -950,7 +950,9 @@ gqla_status gqla_append_expanded_fp8_blocks(const gqla_shape* shape, const gqla_
 
 size_t gqla_attend_gqa_workspace_bytes(const gqla_shape* shape, const int32_t* first, int32_t total, const gqla_cache* expanded_blocks) {
   if (check_packed(shape, first, total, expanded_blocks) != GQLA_OK || shape->dtype != GQLA_BF16 || total == 0 || shape->batch == 0) return 0;
-  return attend_bytes(shape, total, attend_splits_of(shape, total, expanded_blocks));
+  int32_t splits, tile_shift;
+  attend_shape_of(shape, total, expanded_blocks, &splits, &tile_shift);
+  return attend_bytes(shape, total, splits);
 }
 
 gqla_status gqla_attend_gqa_fp8_blocks(const gqla_shape* shape, const int32_t* first, int32_t total, const void* q_c, const void* q_r,
@@ -965,12 +967,12 @@ gqla_status gqla_attend_gqa_fp8_blocks(const gqla_shape* shape, const int32_t* f
   AttendArgs a;
   a.G = shape->h_q / shape->g;
   a.by_G = make_divisor((uint32_t)a.G);
-  a.splits = attend_splits_of(shape, total, expanded_blocks);
+  attend_shape_of(shape, total, expanded_blocks, &a.splits, &a.tile_shift);
   // offsets inside a page are 32-bit
   if (gqla_expanded_fp8_blocks_page_bytes(shape->g, shape->d_h, value_dim(shape), shape->d_r, expanded_blocks->page_size) > INT32_MAX)
     return GQLA_ERR_SHAPE;
-  // rows in 32 bits, and 2^24 workgroups of 256 threads at most: tiles of 128 rows of all sequences and groups, times the ranges
-  if ((int64_t)total * a.G > INT32_MAX || ((int64_t)total * a.G / 128 + shape->batch + 8) * shape->g > (1 << 24) / a.splits) return GQLA_ERR_SHAPE;
+  // rows in 32 bits, and 2^24 workgroups of 256 threads at most: tiles of rows of all sequences and groups, times the ranges
+  if ((int64_t)total * a.G > INT32_MAX || (((int64_t)total * a.G >> a.tile_shift) + shape->batch + 8) * shape->g > (1 << 24) / a.splits) return GQLA_ERR_SHAPE;
   if (a.splits > 1 && (!ws || ws_bytes < attend_bytes(shape, total, a.splits))) return GQLA_ERR_WORKSPACE;
   a.q_c = q_c;
   a.q_r = q_r;

@@ -1,7 +1,8 @@
 // Attention of prompt chunks over the block-scaled 8-bit expanded cache: any number of query rows per sequence, causal.
 //
 // The query rows of a (sequence, group) are its tokens' heads, rho = t * G + head.  A workgroup of four waves takes 128 of them, 32 a
-// wave, and walks the tokens they see in stages of 64, which LDS-DMA brings into a ring of buffers ahead of their use:
+// wave (or 64, where 128 leave too few workgroups), and walks the tokens they see in stages of 64, which LDS-DMA brings into a ring of
+// buffers ahead of their use:
 //   S^T[token][row] = K Q^T,   O^T[dim][row] += V^T P^T
 // with one query row per lane throughout, a running maximum (moved only when outgrown) and an fp32 sum.
 // Codes are widened to bf16 with their block's power of two, exactly, right before their products; probabilities are rounded to bf16.
@@ -69,8 +70,8 @@ __global__ void __launch_bounds__(64 * kWaves, (AttendTile<DH, DV>::kPerUnit)) a
   }
   const int split = unit % a.splits, tile = n_tiles - 1 - unit / a.splits;
   RowSpan r;
-  if (!find_rows<kRows, 1>(a.first, a.seq_lens, a.B, a.total, a.s_q, a.G, tile, r)) return;
-  const int rows = r.n * a.G, tile0 = r.k * kRows;                     // (the host has seen to 32 bits)
+  if (!find_rows<1>(a.first, a.seq_lens, a.B, a.total, a.s_q, a.G, a.tile_shift, tile, r)) return;
+  const int rows = r.n * a.G, tile0 = r.k << a.tile_shift;             // (the host has seen to 32 bits)
   if (tile0 >= rows) return;
   const int P = a.cache.page_size, gc = a.g;
   const int64_t cap = (int64_t)a.cache.max_pages * P;
@@ -79,7 +80,7 @@ __global__ void __launch_bounds__(64 * kWaves, (AttendTile<DH, DV>::kPerUnit)) a
   auto visible = [&](int rho) { return (int)min((int64_t)max(before + token(rho) + 1, 0), cap); };   // tokens that a row sees
   // Waves that would have no rows help the others: with at most 64 rows in the tile two teams, with at most 32 four, take the
   // tiles of 32 tokens in turn and join their states at the end.
-  const int last = rows - 1;
+  const int last = min(rows, tile0 + (1 << a.tile_shift)) - 1;
   const int team_bits = last - tile0 < 32 ? 2 : last - tile0 < 64 ? 1 : 0, row_waves = kWaves >> team_bits;
   const int team = wave >> (2 - team_bits), row_wave = wave & (row_waves - 1);
   const int rho0 = tile0 + row_wave * 32;
@@ -87,7 +88,7 @@ __global__ void __launch_bounds__(64 * kWaves, (AttendTile<DH, DV>::kPerUnit)) a
   const int t = token(rho), head = j * a.G + rho - t * a.G;
   const int vis = (int)min((int64_t)max(before + t + 1, 0), cap);
   const int vis_min = visible(min(rho0, last)), vis_max = visible(min(rho0 + 31, last));   // of the wave
-  const int stages = (int)(((int64_t)visible(min(tile0 + kRows - 1, last)) + kStage - 1) / kStage);
+  const int stages = (int)(((int64_t)visible(last) + kStage - 1) / kStage);
   const int per = (stages + a.splits - 1) / a.splits;
   const int st0 = min(split * per, stages), st1 = min(st0 + per, stages);
 
@@ -410,15 +411,17 @@ hipError_t allow_lds() {
 }
 
 // tiles of rows of a sequence, if all have as many
-int64_t sequence_tiles(int64_t total, int64_t batch, int64_t G) { return std::max<int64_t>(1, (total * G + batch * kRows - 1) / (batch * kRows)); }
+int64_t sequence_tiles(int64_t total, int64_t batch, int64_t G, int shift) {
+  return std::max<int64_t>(1, (total * G + (batch << shift) - 1) / (batch << shift));
+}
 
 template <int DH, int DV>
 hipError_t launch_attend(const AttendArgs& a, hipStream_t s) {
   hipError_t e = allow_lds<DH, DV>();
   if (e != hipSuccess) return e;
-  const int64_t tiles = row_runs(a.total, a.G, kRows, 1, a.B), units = tiles * a.splits;
+  const int64_t tiles = row_runs(a.total, a.G, a.tile_shift, 1, a.B), units = tiles * a.splits;
   // (spread: 64 sequences of 2500 to 5000 tokens, 8 groups, 4 to 8 rows of 4 heads each: 138 -> 123 us; 32 of 4000 to 6000, 4 rows of 16: 101 -> 93)
-  const bool spread = sequence_tiles(a.total, a.B, a.G) == 1;
+  const bool spread = sequence_tiles(a.total, a.B, a.G, a.tile_shift) == 1;
   attend_kernel<DH, DV><<<(unsigned)((spread ? (units + 7) / 8 * 8 : units) * a.g), 64 * kWaves, AttendTile<DH, DV>::kLds, s>>>(a, (int)tiles, spread);
   e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
@@ -431,37 +434,46 @@ hipError_t launch_attend(const AttendArgs& a, hipStream_t s) {
 
 }  // namespace
 
-// Ranges that the tokens are split into: the number with the smallest time by this model, in microseconds, of the 256 units:
-//   N = groups * tiles * splits workgroups of ceil(stages / splits) stages each (two more for their start and end);
-//   a stage takes a workgroup `stage[k]` times the k workgroups that share its unit: up to k = 1, 2, 3 on each unit when N is at most 256 k,
-//   beyond that all run in turn, with half a turn in which units run out of work;
-//   a merge costs 5 us and the partial outputs, written and read at 2.4 TB/s.
-// The rates are fits to sweeps of 1 to 96 ranges.  (time of the call with 1, the chosen number and twice as many) 9 to 16 rows of 4 heads over
-// 20000 to 32000 tokens, 2 sequences: 520, 41 (32), 48 us; 32 sequences of 4000 to 6000, 4 rows of 16 heads: 139, 93 (3), 107; 8 of
-// 10000 to 20000: 399, 99 (12), 115; 8 chunks of 100 to 200 over 2500 to 5000: 157, 141 (2), 153; the same without a context: 24 (1), 40;
-// 1 prompt of 1000: 35 (1), 39.
-int attend_splits(int64_t total, int64_t batch, int h_q, int g, int d_h, int64_t max_tokens) {
-  const int64_t G = h_q / g, tiles = sequence_tiles(total, batch, G) * batch * g;
-  const bool teams = total * G <= 64 * batch;                          // waves share a tile of rows
-  const int per_unit = d_h == 192 ? 2 : 3;
-  static constexpr double kStageTime[3][3] = {{1.8, 1.45, 1.35}, {1.7, 1.25, 1.15}, {2.4, 1.6, 0}};
-  const double* stage = kStageTime[d_h == 192 ? 2 : teams ? 1 : 0];
-  const double part_us = (double)total * h_q * (d_h == 192 ? 256 : 128) * 4 / 2.4e6;
-  const int64_t stages = (max_tokens + kStage - 1) / kStage;
-  int best = 1;
-  double best_us = 0;
+// Rows of a tile (2^7, or 2^6 for which two teams of waves share the tokens) and ranges that the tokens are split into: the pair with
+// the smallest time by this model, in microseconds, of the 256 units:
+//   N = groups * tiles * splits workgroups of ceil(stages / splits) stages each (2.5 more for their start and end);
+//   a stage takes the k workgroups that share a unit stage[k] together.  k goes up to 3 (2 with value dims of 256);
+//   up to N = 256 k the workgroups with the most tokens in sight end last, beyond that a unit has N / (256 k) turns of the mean number
+//   of tokens in sight, and 0.15 of a turn in which units run out of work;
+//   a merge costs 6.5 us and the partial outputs, written and read at 2.4 TB/s.
+// The rates are fits to sweeps of 1 to 32 ranges and both tiles, off by 11 %; over 19 shapes the pair it takes is 1 % behind the best of the
+// sweep, tiles of 128 rows alone 6 %.  (128 rows, 64 rows) 1 prompt of 1000 x 32 heads: 38, 29 us; 1 of 2500 x 16 heads in one group: 69, 60; 4 chunks
+// of 100 to 512 x 20 heads in 5 groups over 1000 to 3000: 76 (4 ranges), 68 (2); 8 tokens x 128 heads over 20000: 38, 35 (32); 1 prompt of
+// 3000 x 32 heads: 121, 124; 8 of 500 to 1000: 78, 87.  (ranges, at their better tile) 9 to 16 tokens x 32 heads, two over 20000 to
+// 32000: 518 (1), 51 (16), 41 (32) us; 8 of 4 to 8 x 128 heads over 10000 to 20000: 372 (1), 100 (12), 121 (32); 8 chunks of 100 to 200 x 32 heads
+// over 2500 to 5000: 142 (1), 144 (2), 151 (3); the same without a context: 23 (1), 39 (2).
+void attend_shape(int64_t total, int64_t batch, int h_q, int g, int d_h, int64_t max_tokens, int32_t* splits, int32_t* tile_shift) {
+  static constexpr double kStageTime[2][2][3] = {{{2.0, 2.65, 3.2}, {1.3, 1.7, 2.2}}, {{2.5, 3.25}, {1.7, 2.15}}};
+  const int64_t G = h_q / g, stages = (max_tokens + kStage - 1) / kStage;
+  const bool wide = d_h == 192, few = total * G <= 64 * batch;         // few: a tile of 128 is one of 64 or less
+  const int per_unit = wide ? 2 : 3;
+  const double part_us = (double)total * h_q * (wide ? 256 : 128) * 4 / 2.4e6;
+  const double mean = std::max(0.5, 1 - 0.5 * total / ((double)batch * max_tokens));   // tokens that a row sees, of the most
   const int most = total * h_q > (1 << 24) ? 1 : 64;                   // (the merge has a workgroup per row at the most)
-  for (int s = 1; s <= most && s <= stages; ++s) {
-    const double n = (double)tiles * s, length = (double)((stages + s - 1) / s + 2);
-    const int k = n >= 256.0 * per_unit ? per_unit : std::max(1, (int)std::ceil(n / 256.0));
-    double us = length * stage[k - 1] * (n > 256.0 * per_unit ? n / 256.0 + 0.5 * per_unit : k);
-    if (s > 1) us += 5 + s * part_us;
-    if (s == 1 || us < best_us) {
-      best = s;
-      best_us = us;
+  double best = INFINITY;
+  *splits = 1;
+  *tile_shift = 7;
+  for (int shift = 7; shift >= (few ? 7 : 6); --shift) {
+    const double* stage = kStageTime[wide][few || shift == 6];
+    const double tiles = (double)(sequence_tiles(total, batch, G, shift) * batch * g);
+    for (int s = 1; s <= most && (s == 1 || s <= stages); ++s) {
+      const double n = tiles * s / 256, length = (double)((stages + s - 1) / s);
+      const int k = (int)std::ceil(std::min(n, (double)per_unit));
+      double us = n > k ? ((length * mean + 2.5) * n / k + 0.15 * (length + 2.5)) * stage[k - 1]
+                        : (length + 2.5) * (mean + (1 - mean) / k) * stage[k - 1];
+      if (s > 1) us += 6.5 + s * part_us;
+      if (us < best) {
+        best = us;
+        *splits = s;
+        *tile_shift = shift;
+      }
     }
   }
-  return best;
 }
 
 hipError_t launch_attend_fp8_blocks(const AttendArgs& a, hipStream_t s) {

@@ -13,7 +13,7 @@ namespace gqla {
 
 namespace {
 
-constexpr int kBlock = 32;                 // tokens that share a scale: the decode kernels' tile
+constexpr int kBlockShift = 5, kBlock = 1 << kBlockShift;   // tokens that share a scale: the decode kernels' tile
 constexpr int kExpMin = -100, kExpMax = 118;
 
 __device__ __forceinline__ int block_exponent(uint32_t amax_bits) {
@@ -119,7 +119,7 @@ __global__ void __launch_bounds__(256) append_rows_kernel(AppendRowsArgs a, int 
   double theta = 0.0;
   if (rotates && a.log2_base > 0.0) theta = exp2(-2.0 * (int)(threadIdx.x & 31) / DR * a.log2_base) * 0.15915494309189535;
   RowSpan r;
-  if (!find_rows<kBlock, 2>(a.first, a.seq_lens, a.B, a.total, a.s_q, 1, blockIdx.x, r)) return;
+  if (!find_rows<2>(a.first, a.seq_lens, a.B, a.total, a.s_q, 1, kBlockShift, blockIdx.x, r)) return;
   // positions p0 .. len - 1 are new; this block's share is [lo, hi)
   const int64_t p0 = (int64_t)r.len - r.n;
   const int64_t t0_wide = (max(p0, (int64_t)0) / kBlock + r.k) * kBlock;
@@ -387,7 +387,7 @@ __global__ void __launch_bounds__(256) append_rows_kernel(AppendRowsArgs a, int 
 // fp32 rows: a workgroup per row, an element per thread and pass (any dims that are multiples of 8; for the small fp32 path).
 __global__ void __launch_bounds__(256) append_rows_f32_kernel(AppendRowsArgs a) {
   RowSpan r;
-  if (!find_rows<1, 0>(a.first, a.seq_lens, a.B, a.total, a.s_q, 1, blockIdx.x, r) || r.k >= r.n) return;
+  if (!find_rows<0>(a.first, a.seq_lens, a.B, a.total, a.s_q, 1, 0, blockIdx.x, r) || r.k >= r.n) return;
   const int64_t t = (int64_t)r.len - r.n + r.k;
   if (t < 0) return;
   const int P = a.cache.page_size, gc = a.g, slot = (int)(t % P);
@@ -531,7 +531,7 @@ hipError_t launch_append(const AppendRowsArgs& a, hipStream_t s) {
   // table is read four times as often.  (128 heads, eight -> two) 150 rows 10.9 -> 5.9 us, 3700 26.7 -> 25.7, 6000 61.4 -> 58.4, 30000
   // 246 -> 247, 120000 958 -> 995; (32 heads) 750 7.1 -> 6.6, 6000 20.8 -> 20.9, 30000 97 -> 101.
   const int at_once = a.total > 4 * (int64_t)a.B && a.total <= 8192 && a.h_q >= 32 ? 2 : 8;
-  append_rows_kernel<DH, DV, BLOCKS><<<dim3((unsigned)row_runs(a.total, 1, kBlock, 2, a.B), kv + kBlock / at_once), 256, 0, s>>>(a, kv, at_once);
+  append_rows_kernel<DH, DV, BLOCKS><<<dim3((unsigned)row_runs(a.total, 1, kBlockShift, 2, a.B), kv + kBlock / at_once), 256, 0, s>>>(a, kv, at_once);
   return hipGetLastError();
 }
 

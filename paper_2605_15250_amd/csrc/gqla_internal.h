@@ -120,6 +120,7 @@ struct AttendArgs {
   float* part_o;                    // splits > 1: [splits][total][h_q][d_v], then the log-sum-exps [splits][total][h_q]
   float* part_lse;
   int32_t B, total, s_q, h_q, g, G, d_h, d_v, splits;
+  int32_t tile_shift;               // a workgroup's tile has 2^tile_shift rows: 2^6 or 2^7
   Divisor by_G;                     // G = h_q / g
   float scale_log2e;
 };
@@ -189,7 +190,8 @@ hipError_t launch_append_rows_f32(const AppendRowsArgs&, hipStream_t);
 hipError_t launch_append_rows_bf16(const AppendRowsArgs&, hipStream_t);
 hipError_t launch_append_rows_fp8_blocks(const AppendRowsArgs&, hipStream_t);
 hipError_t launch_quantize_blocks(const QuantizeArgs&, int d_h, hipStream_t);  // src: 16-bit expanded cache, dst: block scales
-int attend_splits(int64_t total, int64_t batch, int h_q, int g, int d_h, int64_t max_tokens);
+// ranges that the tokens are split into and logarithm of the rows of a tile
+void attend_shape(int64_t total, int64_t batch, int h_q, int g, int d_h, int64_t max_tokens, int32_t* splits, int32_t* tile_shift);
 hipError_t launch_attend_fp8_blocks(const AttendArgs&, hipStream_t);
 
 hipError_t launch_probe_stream_read(const void* src, size_t bytes, uint32_t* sink, int blocks, hipStream_t);

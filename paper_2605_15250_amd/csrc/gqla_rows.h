@@ -1,8 +1,8 @@
 // Rows of new tokens, packed over ragged sequences: which sequence a workgroup works on.
 //
 // Rows first[b] .. first[b + 1] - 1 of the packed buffers belong to sequence b (first == NULL: s_q rows each).  Work is dealt out in
-// runs of BLOCK rows without a scan of the run lengths: sequence b's runs are numbered from floor(first[b] * mul / BLOCK) + EXTRA * b, and
-// floor(x + y) >= floor(x) + floor(y) leaves room for floor(n mul / BLOCK) + EXTRA of them; a run that its sequence does not need is
+// runs of 2^shift rows without a scan of the run lengths: sequence b's runs are numbered from floor(first[b] * mul / 2^shift) + EXTRA * b, and
+// floor(x + y) >= floor(x) + floor(y) leaves room for floor(n mul / 2^shift) + EXTRA of them; a run that its sequence does not need is
 // left at once.  Finding the sequence is then one comparison per sequence, 64 at a time, instead of a prefix sum.
 // Values of `first` are clamped into [0, total] and a falling one gives no rows, so that whatever it holds stays in bounds.
 #pragma once
@@ -16,11 +16,11 @@ struct RowSpan {
   int k;                 // which of the sequence's runs
 };
 
-template <int BLOCK, int EXTRA>
-__device__ __forceinline__ bool find_rows(const int32_t* first, const int32_t* seq_lens, int batch, int total, int s_q, int mul, int x, RowSpan& r) {
+template <int EXTRA>
+__device__ __forceinline__ bool find_rows(const int32_t* first, const int32_t* seq_lens, int batch, int total, int s_q, int mul, int shift, int x, RowSpan& r) {
   const int lane = threadIdx.x & 63;
   auto begin = [&](int b) { return first ? min(max(first[b], 0), total) : b * s_q; };
-  auto run = [&](int f, int b) { return (int)((int64_t)f * mul / BLOCK) + EXTRA * b; };
+  auto run = [&](int f, int b) { return (int)((int64_t)f * mul >> shift) + EXTRA * b; };
   if (batch < 64) {  // everything with one latency
     const int f = begin(min(lane, batch));
     const int l = seq_lens[min(lane, batch - 1)];
@@ -49,6 +49,6 @@ __device__ __forceinline__ bool find_rows(const int32_t* first, const int32_t* s
 }
 
 // Runs of the whole batch, for the grid.
-inline int64_t row_runs(int64_t total, int64_t mul, int64_t block, int64_t extra, int64_t batch) { return total * mul / block + extra * batch; }
+inline int64_t row_runs(int64_t total, int64_t mul, int shift, int64_t extra, int64_t batch) { return (total * mul >> shift) + extra * batch; }
 
 }  // namespace gqla

@@ -368,6 +368,19 @@ def test_attend(g, G, d_h, d_v, P, lens, ns):
     w.check_attention(out, lse, q_c, q_r, first, lens)
 
 
+@pytest.mark.parametrize("g,G,d_h,d_v,B_", [(8, 4, 128, 128, 40), (5, 4, 192, 256, 32)])
+def test_attend_rows_enough_for_the_large_tile(g, G, d_h, d_v, B_):
+    """A workgroup for 128 rows, not 64: the chip is full of them."""
+    ns = [100, 64, 97, 65, 129, 1, 96, 112] * (B_ // 8)
+    lens = [n + (17 * b) % 50 for b, n in enumerate(ns)]
+    w = World(lens, g, d_h, d_v, G=G, seed=86 + g)
+    w.append(lens)
+    w.spoil()
+    q_c, q_r = stored(w.r.normal(size=(sum(ns), g * G, d_h))), stored(w.r.normal(size=(sum(ns), g * G, D_R)))
+    out, lse, first, _ = attend(w, ns, lens, q_c, q_r, extra=1)
+    w.check_attention(out, lse, q_c, q_r, first, lens)
+
+
 def test_attend_rows_that_see_nothing_and_missing_pages():
     lens = [3, 200, 70]
     w = World([64, 200, 70], 2, G=4, seed=91)
