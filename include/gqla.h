@@ -390,7 +390,7 @@ gqla_status gqla_append_expanded_fp8_blocks(const gqla_shape* shape, const gqla_
  * only, max_pages * page_size standing for the longest context, and holds nothing between calls; calls whose kernels can overlap
  * (other streams, graphs replayed side by side) need one each.
  * Errors: GQLA_ERR_WORKSPACE when ws is missing or too small; GQLA_ERR_SHAPE when total * h_q / g exceeds 2^31, the launch 2^24 workgroups
- * (one per 128 query rows of a sequence and group, and per range of the context) or a page 2^31 bytes; others as above. */
+ * (one per 128 query rows, or 64 in small calls, of a sequence and group, and per range of the context) or a page 2^31 bytes; others as above. */
 gqla_status gqla_attend_gqa_fp8_blocks(const gqla_shape* shape, const int32_t* first, int32_t total, const void* q_c, const void* q_r,
                                        const gqla_cache* expanded_blocks, void* out, float* lse, void* ws, size_t ws_bytes,
                                        void* stream);

@@ -98,8 +98,8 @@ __device__ __forceinline__ uint32_t token_bytes(int w, int h, int a, int b) {
 }
 
 // ---- rows of new tokens ----------------------------------------------------------------------------------------------
-// One wave per (sequence, block of 32 positions, group, K or V; 16-bit values of 256 dims are two waves' work): it alone owns what it writes, its scale included, so there is
-// nothing to synchronise.  K: a lane takes one token and every second run of 8 dims, which are output vectors as they are.  V: a lane takes
+// One wave per (sequence, block of 32 positions, group, K or V; 16-bit values of 256 dims are two waves' work): it alone owns what it
+// writes, its scale included, so there is nothing to synchronise.  K: a lane takes one token and every second run of 8 dims, which are output vectors as they are.  V: a lane takes
 // 4 dims (8 of 256 as codes) and the 16 tokens of an output vector, so that a load covers whole rows of two tokens and the turn from
 // token-major to dim-major happens in registers; vectors that others share are stored element by element or, as codes, read, changed and
 // written back.  At most four new tokens (a step): a lane takes four dims of each, and codes are stored byte by byte, with no read of
@@ -107,6 +107,8 @@ __device__ __forceinline__ uint32_t token_bytes(int w, int h, int a, int b) {
 // More workgroups per block take 8 tokens each, or 2, and rotate: one sine and cosine per (token, pair) in LDS, shared by k_R and all
 // heads of the queries; the angle is formed and reduced in double.
 // Bound by HBM for prompts and by latency for a step: row bounds and lengths -> page (the rows on their way beside it) -> old scale -> stores.
+// Eight ragged prompts of 500 to 4000 tokens, 8 groups: 56 us = 4.6 TB/s read and written (a copy reaches 4.95); 4 of 300 to
+// 3000 into the 16-bit cache, (192, 256): 20.5 us; 64 sequences' two tokens x 128 heads 6.8 us; one token 3.8 us.
 constexpr int kFew = 4;
 
 template <int DH, int DV, bool BLOCKS>
@@ -427,6 +429,7 @@ __global__ void __launch_bounds__(256) append_rows_f32_kernel(AppendRowsArgs a) 
 // ---- 16-bit expanded cache -> block scales ----------------------------------------------------------------------------------
 // One wave per (page, tile of 32 tokens, group, K or V), a wave per tile for k_R behind them.  Both formats are made of
 // vectors in the same order, so that loads and stores are runs of whole vectors.  Only bytes that belong to tokens t < L are written.
+// Bound by HBM: 32 ragged sequences of 2049 to 6143 tokens, 8 groups (817 MB read and written) 168 us = 4.85 TB/s; 333 tokens 6 us.
 template <int DH, int DV>
 __global__ void __launch_bounds__(256) quantize_blocks_kernel(QuantizeArgs a) {
   constexpr int DR = 64;

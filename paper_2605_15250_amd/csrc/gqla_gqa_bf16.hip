@@ -49,7 +49,8 @@ __device__ __forceinline__ bf16x8 widen_e4m3(uint32_t w0, uint32_t w1, float sca
 // BLK (8-bit codes): a power of two per (32 tokens, group) for K and for V instead of k_scale and v_scale.  A tile's pair comes
 // through the scalar cache with the request of its codes and enters where they are widened, at no instruction.  The
 // denominator sums the probabilities ahead of their rounding to bf16 (which saves unpacking them: 2^-9 of each, at random, stays in the
-// output, and the log-sum-exp is as exact as fp32 has it).
+// output, and the log-sum-exp is as exact as fp32 has it).  64 sequences of 8192 tokens x 128 heads, two rows: 172 us = 6.7 TB/s, as
+// with one scale (170); one sequence of 1000 tokens x 32 heads 6.7 us.
 template <int DH, int DV, int DR, bool FP8, int MAXT, int RB, bool TEAM, bool DEEP, bool BLK = false>
 __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int n_items, int row_blocks, int share_kr_arg,
                                                                int tt_arg, float k_scale, float v_scale) {
