@@ -105,10 +105,6 @@ __global__ void __launch_bounds__(64 * kWaves, (AttendTile<DH, DV>::kPerUnit)) a
 #pragma unroll
     for (int ks = 0; ks < KR; ++ks) qr[ks] = *(const bf16x8*)(pr + 16 * ks);
   }
-#pragma unroll
-  for (int ks = 0; ks < 2 * KC; ++ks) asm volatile("" : "+v"(qc[ks]));
-#pragma unroll
-  for (int ks = 0; ks < KR; ++ks) asm volatile("" : "+v"(qr[ks]));      // (waited for here: a wait inside the loop would be one for the requests, too)
 
   // Where this wave's pieces of a stage begin in a page (32 bits: the host has seen to that), for its first slots; a stage further on
   // in the page adds 64 vectors of 16 bytes to those of K and k_R, 64 * DV bytes to those of V.
@@ -161,6 +157,19 @@ __global__ void __launch_bounds__(64 * kWaves, (AttendTile<DH, DV>::kPerUnit)) a
   auto scales_of = [&](Stage g) -> f32x4 {                              // K, V of the stage's first tile, K, V of its second
     return *(const_f32x4_ptr)(uintptr_t)(page_of_stage(g) + scale_off + g.slot / 32 * 8);
   };
+
+  Stage here = {-1, 0}, next = here;                                   // this stage; the next one, looked up a stage ahead of its request
+  f32x4 sc = {1.f, 1.f, 1.f, 1.f};
+  if (st0 < st1) {                                                     // the first stage comes while the queries do
+    here = look_up();
+    request(here, 0);
+    sc = scales_of(here);
+    if (st0 + 1 < st1) next = look_up();
+  }
+#pragma unroll
+  for (int ks = 0; ks < 2 * KC; ++ks) asm volatile("" : "+v"(qc[ks]));
+#pragma unroll
+  for (int ks = 0; ks < KR; ++ks) asm volatile("" : "+v"(qr[ks]));      // (waited for here: a wait inside the loop would be one for the requests, too)
 
   f32x16 o[MT];
 #pragma unroll
@@ -225,41 +234,35 @@ __global__ void __launch_bounds__(64 * kWaves, (AttendTile<DH, DV>::kPerUnit)) a
     }
   };
 
-  if (st0 < st1) {
-    Stage here = look_up(), next = here;                               // this stage; the next one, looked up a stage ahead of its request
-    if (st0 + 1 < st1) next = look_up();
-    request(here, 0);
-    f32x4 sc = scales_of(here);
-    for (int st = st0; st < st1; ++st) {
-      const int buf = (st - st0) & 1;
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      __syncthreads();                                                 // every wave's share is there; the other buffer is free
-      if (st + 1 < st1) request(next, buf ^ 1);
-      const bool there = here.page >= 0;
-      here = next;
-      const f32x4 now = sc;
-      if (st + 1 < st1) sc = scales_of(here);
-      if (st + 2 < st1) next = look_up();
-      const int tok = st * kStage;
-      if (there && r.len - tok < kStage) {   // the sequence ends here: value codes behind it may be anything (NaN included), a weight of 0 is not enough
-        char* vectors = smem + (buf * PIECES + 2 * (KC + KR)) * 1024 + lane * 16;
-        for (int p = wave; p < 2 * MT; p += kWaves) {
-          u32x4 v = *(const u32x4*)(vectors + p * 1024);
+  for (int st = st0; st < st1; ++st) {
+    const int buf = (st - st0) & 1;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();                                                   // every wave's share is there; the other buffer is free
+    if (st + 1 < st1) request(next, buf ^ 1);
+    const bool there = here.page >= 0;
+    here = next;
+    const f32x4 now = sc;
+    if (st + 1 < st1) sc = scales_of(here);
+    if (st + 2 < st1) next = look_up();
+    const int tok = st * kStage;
+    if (there && r.len - tok < kStage) {   // the sequence ends here: value codes behind it may be anything (NaN included), a weight of 0 is not enough
+      char* vectors = smem + (buf * PIECES + 2 * (KC + KR)) * 1024 + lane * 16;
+      for (int p = wave; p < 2 * MT; p += kWaves) {
+        u32x4 v = *(const u32x4*)(vectors + p * 1024);
 #pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (tok + p / MT * 32 + 16 * (e >> 3) + 8 * h + (e & 7) >= r.len) v[e >> 2] &= ~(0xffu << (8 * (e & 3)));
-          *(u32x4*)(vectors + p * 1024) = v;
-        }
-        __syncthreads();
+        for (int e = 0; e < 16; ++e)
+          if (tok + p / MT * 32 + 16 * (e >> 3) + 8 * h + (e & 7) >= r.len) v[e >> 2] &= ~(0xffu << (8 * (e & 3)));
+        *(u32x4*)(vectors + p * 1024) = v;
       }
-      if (there) {                                                     // a page that is not there holds nothing
-        const char *ring = smem + buf * (PIECES * 1024), *keys = ring + key_lane, *vals = ring + 2 * (KC + KR) * 1024 + lane * 16;
-        // tile q of 32 tokens is team q mod teams's
-        const int teams = 1 << team_bits, first = 2 * st & (teams - 1);
-        if (tok < vis_max && team == first) attend_tile(tok, keys, keys + 2 * KC * 1024, vals, now[0], now[1]);
-        if (tok + 32 < vis_max && team == (first + 1 & (teams - 1)))
-          attend_tile(tok + 32, keys + KC * 1024, keys + (2 * KC + KR) * 1024, vals + MT * 1024, now[2], now[3]);
-      }
+      __syncthreads();
+    }
+    if (there) {                                                       // a page that is not there holds nothing
+      const char *ring = smem + buf * (PIECES * 1024), *keys = ring + key_lane, *vals = ring + 2 * (KC + KR) * 1024 + lane * 16;
+      // tile q of 32 tokens is team q mod teams's
+      const int teams = 1 << team_bits, first = 2 * st & (teams - 1);
+      if (tok < vis_max && team == first) attend_tile(tok, keys, keys + 2 * KC * 1024, vals, now[0], now[1]);
+      if (tok + 32 < vis_max && team == (first + 1 & (teams - 1)))
+        attend_tile(tok + 32, keys + KC * 1024, keys + (2 * KC + KR) * 1024, vals + MT * 1024, now[2], now[3]);
     }
   }
   // the teams' states become one, half of them at a time
