@@ -4,7 +4,8 @@
 // runs of 2^shift rows without a scan of the run lengths: sequence b's runs are numbered from floor(first[b] * mul / 2^shift) + EXTRA * b, and
 // floor(x + y) >= floor(x) + floor(y) leaves room for floor(n mul / 2^shift) + EXTRA of them; a run that its sequence does not need is
 // left at once.  Finding the sequence is then one comparison per sequence, 64 at a time, instead of a prefix sum.
-// Values of `first` are clamped into [0, total] and a falling one gives no rows, so that whatever it holds stays in bounds.
+// Values of `first` are clamped into [0, total], and where one falls the count of sequences at or before x may name one behind x (k < 0) or
+// one without rows: neither is worked on, so that whatever `first` holds stays in bounds.
 #pragma once
 
 #include "gqla_device.h"
@@ -45,7 +46,7 @@ __device__ __forceinline__ bool find_rows(const int32_t* first, const int32_t* s
     r.len = __builtin_amdgcn_readfirstlane(seq_lens[r.b]);
   }
   r.k = x - run(r.first, r.b);
-  return r.n > 0;
+  return r.n > 0 && r.k >= 0;
 }
 
 // Runs of the whole batch, for the grid.

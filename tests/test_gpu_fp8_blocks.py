@@ -381,6 +381,35 @@ def test_attend_rows_enough_for_the_large_tile(g, G, d_h, d_v, B_):
     w.check_attention(out, lse, q_c, q_r, first, lens)
 
 
+@pytest.mark.parametrize("B_", [4, 70])
+def test_row_bounds_that_fall_stay_in_bounds(B_):
+    """`first` is the caller's; whatever it holds, nothing ahead of or behind the buffers is written."""
+    g, G, total, guard = 2, 4, 1200, 2000
+    w = World([64] * B_, g, G=G, seed=95)
+    w.append([40] * B_)
+    bad = np.zeros(B_ + 1, np.int32)
+    bad[1:3] = 1000, 1100                                 # sequence 1 has rows, the ones behind it begin at 0 again
+    bad[-1] = -5
+    d_first = torch.from_numpy(bad).cuda()
+    heads = g * G
+    rows = lambda d: torch.full((total + 2 * guard, heads, d), 7.0, dtype=torch.bfloat16, device="cuda")  # noqa: E731
+    q_c, q_r, q_rot, out = rows(128), rows(D_R), rows(D_R), rows(128)
+    lse = torch.full((total + 2 * guard, heads), 7.0, device="cuda")
+    mid = slice(guard, guard + total)
+    w.sync_lens([64] * B_)
+    cache = w.cache()
+    need = B.gqla_attend_gqa_workspace_bytes(w.shape, d_first, total, cache)
+    ws = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
+    B.gqla_attend_gqa_fp8_blocks(w.shape, d_first, total, q_c[mid], q_r[mid], cache, out[mid], lse[mid], ws)
+    k, v = (torch.zeros((total, g, 128), dtype=torch.bfloat16, device="cuda") for _ in "kv")
+    k_r = torch.zeros((total, D_R), dtype=torch.bfloat16, device="cuda")
+    new = B.make_new_rows(k, v, k_r, q_r[mid], q_rot[mid], d_first, total)
+    B.gqla_append_expanded_fp8_blocks(w.shape, new, BASE, cache)
+    torch.cuda.synchronize()
+    for x in (out, lse, q_rot):
+        assert bool((x[:guard] == 7.0).all()) and bool((x[guard + total:] == 7.0).all())
+
+
 def test_attend_rows_that_see_nothing_and_missing_pages():
     lens = [3, 200, 70]
     w = World([64, 200, 70], 2, G=4, seed=91)
