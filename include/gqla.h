@@ -373,7 +373,7 @@ typedef struct {
  * larger of its own exponent and the one that the new rows need; where it grows, the older codes are rounded to the new
  * scale (exact but for codes that fall below E4M3's normal range).  Appending the same rows again changes nothing.
  * Errors: GQLA_ERR_SHAPE for another group count, rope_base, total < 0, total > 2^23, batch > 2^20, d_r odd or above 512; GQLA_ERR_NULL for q_r without
- * q_rot or the reverse; others as for gqla_append_latent.  Both calls only enqueue one kernel on `stream`. */
+ * q_rot or the reverse (not where total = 0); others as for gqla_append_latent.  Both calls only enqueue one kernel on `stream`. */
 gqla_status gqla_append_expanded(const gqla_shape* shape, const gqla_new_rows* rows, float rope_base, const gqla_cache* expanded,
                                  void* stream);
 gqla_status gqla_append_expanded_fp8_blocks(const gqla_shape* shape, const gqla_new_rows* rows, float rope_base,

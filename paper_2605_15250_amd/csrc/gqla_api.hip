@@ -891,7 +891,8 @@ gqla_status append_impl(const gqla_shape* shape, const gqla_new_rows* rows, floa
   gqla_status st = check_packed(shape, rows->first, rows->total, expanded);
   if (st != GQLA_OK) return st;
   if (blocks && shape->dtype != GQLA_BF16) return GQLA_ERR_DTYPE;
-  if (!rows->k_c || !rows->v || !rows->k_r || !rows->q_r != !rows->q_rot) return GQLA_ERR_NULL;
+  const bool some = shape->batch > 0 && rows->total > 0;               // (buffers of no rows have no address)
+  if (some && (!rows->k_c || !rows->v || !rows->k_r || !rows->q_r != !rows->q_rot)) return GQLA_ERR_NULL;
   if (!aligned16(rows->k_c) || !aligned16(rows->v) || !aligned16(rows->k_r) || !aligned16(rows->q_r) || !aligned16(rows->q_rot))
     return GQLA_ERR_ALIGN;
   if (!(rope_base == 0.0f || (rope_base > 1.0f && std::isfinite(rope_base))) || shape->d_r % 2 || shape->d_r > 512) return GQLA_ERR_SHAPE;
@@ -907,7 +908,7 @@ gqla_status append_impl(const gqla_shape* shape, const gqla_new_rows* rows, floa
   a.v_stride = stride(rows->v_stride, shape->g * d_v);
   a.kr_stride = stride(rows->kr_stride, shape->d_r);
   if (st != GQLA_OK) return st;
-  if (shape->batch == 0 || rows->total == 0) return GQLA_OK;
+  if (!some) return GQLA_OK;
   a.k_c = rows->k_c;
   a.v = rows->v;
   a.k_r = rows->k_r;
@@ -961,9 +962,10 @@ gqla_status gqla_attend_gqa_fp8_blocks(const gqla_shape* shape, const int32_t* f
   gqla_status st = check_packed(shape, first, total, expanded_blocks);
   if (st != GQLA_OK) return st;
   if (shape->dtype != GQLA_BF16) return GQLA_ERR_DTYPE;
-  if (!q_c || !q_r || !out) return GQLA_ERR_NULL;
+  const bool some = shape->batch > 0 && total > 0;
+  if (some && (!q_c || !q_r || !out)) return GQLA_ERR_NULL;
   if (!aligned16(q_c) || !aligned16(q_r) || !aligned16(out) || !aligned16(ws) || (reinterpret_cast<uintptr_t>(lse) & 3u)) return GQLA_ERR_ALIGN;
-  if (shape->batch == 0 || total == 0) return GQLA_OK;
+  if (!some) return GQLA_OK;
   AttendArgs a;
   a.G = shape->h_q / shape->g;
   a.by_G = make_divisor((uint32_t)a.G);

@@ -460,7 +460,7 @@ void attend_shape(int64_t total, int64_t batch, int h_q, int g, int d_h, int64_t
   const int per_unit = wide ? 2 : 3;
   const double part_us = (double)total * h_q * (wide ? 256 : 128) * 4 / 2.4e6;
   const double mean = std::max(0.5, 1 - 0.5 * total / ((double)batch * max_tokens));   // tokens that a row sees, of the most
-  const int most = total * h_q > (1 << 24) ? 1 : 64;                   // (the merge has a workgroup per row at the most)
+  const int most = total * h_q >= (1 << 24) ? 1 : 64;                  // (the merge has a workgroup per row at the most)
   double best = INFINITY;
   *splits = 1;
   *tile_shift = 7;

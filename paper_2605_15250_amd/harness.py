@@ -235,7 +235,8 @@ class Decoder:
         """New rows k_c [n, groups * d_h], v [n, groups * d_v], k_r [n, d_r] (unit stride inside a row) into the expanded cache, or into the
         one with block scales; returns the rotated queries.  first: device int32 [B + 1], None: s_q rows per sequence."""
         q_rot = torch.empty_like(q_r) if q_r is not None else None
-        rows = B.make_new_rows(k_c, v, k_r, q_r, q_rot, first, k_c.shape[0], k_c.stride(0), v.stride(0), k_r.stride(0))
+        n = k_c.shape[0]
+        rows = B.make_new_rows(k_c, v, k_r, q_r, q_rot, first, n, *(x.stride(0) if n > 1 else 0 for x in (k_c, v, k_r)))   # (one row: no stride)
         if blocks:
             B.gqla_append_expanded_fp8_blocks(self.shape_gqa, rows, rope_base, self.expanded_blocks_cache())
         else:

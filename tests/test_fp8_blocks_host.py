@@ -112,6 +112,16 @@ def test_append_refusals(fn):
     call(shape=_shape(batch=0, s_q=2), rows=_rows(first=None, total=0))
 
 
+def test_calls_without_rows_take_buffers_without_an_address():
+    """An empty tensor's address is NULL: a step in which no sequence has a new token."""
+    none = _rows(k_c=None, v=None, k_r=None, total=0)
+    for fn in (B.gqla_append_expanded, B.gqla_append_expanded_fp8_blocks):
+        fn(_shape(), none, 1e4, _cache(), stream=0)
+        fn(_shape(), _rows(k_c=None, v=None, k_r=None, q_r=A, total=0), 1e4, _cache(), stream=0)
+    B.gqla_attend_gqa_fp8_blocks(_shape(), A, 0, None, None, _cache(), None, None, None, 0, stream=0)
+    _refused(B.GQLA_ERR_ALIGN, B.gqla_attend_gqa_fp8_blocks, _shape(), A, 0, A + 8, None, _cache(), None, None, None, 0, stream=0)
+
+
 def test_quantize_and_decode_refusals():
     q = lambda shape=_shape(), a=_cache(), b=_cache(): B.gqla_quantize_expanded_fp8_blocks(shape, a, b, stream=0)  # noqa: E731
     _refused(B.GQLA_ERR_DTYPE, q, shape=_shape(d_h=16, dtype=B.GQLA_F32))

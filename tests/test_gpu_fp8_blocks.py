@@ -606,3 +606,32 @@ def test_decoder_from_the_cache_switch():
         assert float((lse.view(4, -1) - lse2).abs().max()) <= 1e-4
     finally:
         case.close()
+
+
+def test_decoder_takes_one_row_and_none():
+    """A tensor of one row may name any stride; one of none has no address."""
+    import synth_inputs as S
+    from test_gpu_parity import Case
+    cfg = S.CONFIGS["C3"].with_(B=1, L=0, s_q=1, paged=True, seed=991)
+    case = Case(cfg, lens=[40])
+    dec = case.dec
+    try:
+        row = lambda d: torch.randn(d, device="cuda").to(torch.bfloat16)  # noqa: E731
+        k, v, kr = row(cfg.g * cfg.d_h), row(cfg.g * cfg.d_h), row(cfg.d_r)
+        pools = []
+        for odd in (False, True):
+            shaped = [torch.as_strided(x, (1, x.numel()), (1, 1)) if odd else x.view(1, -1) for x in (k, v, kr)]
+            pool = dec.alloc_expanded_blocks()
+            dec.append_expanded(BASE, *shaped, blocks=True)
+            pools.append(pool)
+        torch.cuda.synchronize()
+        assert bool((pools[0] != 0xAA).any()) and torch.equal(*pools)
+        before = pools[1].clone()
+        none = lambda *s: torch.empty(s, dtype=torch.bfloat16, device="cuda")  # noqa: E731
+        first = torch.zeros(2, dtype=torch.int32, device="cuda")
+        q_rot = dec.append_expanded(BASE, none(0, cfg.g * cfg.d_h), none(0, cfg.g * cfg.d_h), none(0, cfg.d_r), none(0, cfg.h_q, cfg.d_r), first, blocks=True)
+        out, lse = dec.attend_gqa_blocks(none(0, cfg.h_q, cfg.d_h), q_rot, first)
+        torch.cuda.synchronize()
+        assert out.shape == (0, cfg.h_q, cfg.d_h) and torch.equal(pools[1], before)
+    finally:
+        case.close()
