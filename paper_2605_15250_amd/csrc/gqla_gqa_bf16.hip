@@ -261,8 +261,9 @@ __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int
           for (int i = 0; i < 16; ++i) s[i] *= k_scale;
         }
         // behind this tile's k_R (loads complete in issue order): its key and value codes and the next tile's
-        static_assert(KS_C + 2 * MT == 16, "the wait below is written for this count");
-        asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
+        static_assert(KS_C + 2 * MT == 16 || KS_C + 2 * MT == 28, "the wait below is written for these counts");
+        if constexpr (KS_C + 2 * MT == 16) asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
+        else asm volatile("s_waitcnt vmcnt(28)" ::: "memory");
         __syncthreads();
         const char* kr = kr_lds[slot] + lane * 16;
 #pragma unroll
@@ -834,7 +835,10 @@ static hipError_t launch_decode_gqa_128(const DecodeArgs& a, float k_scale, floa
   return hipGetLastError();
 }
 
-// (d_h, d_v) = (192, 256): four waves per workgroup, one row block each
+// (d_h, d_v) = (192, 256): four waves per workgroup, one row block each.  A wave is alone on its SIMD, and 15 KB of codes in flight are not enough:
+// codes take two tiles where four waves share k_R and chunks are long enough.  One tile over two (time of the call; 1 to 8 x 256 CUs' waves'
+// worth of items, 4 to 32 rows a group): chunks of 2 tiles 0.93 to 0.96, 4 0.98 to 0.99, 6 1.02 to 1.06, 8 1.05, 14 1.12, 32 and more 1.10 to
+// 1.15 (64 x 8000 tokens, 8 groups: 333 -> 304 us = 6.3 TB/s; 4 groups 194 -> 176).  Two groups, whose workgroups have two waves: 0.94 to 1.01.
 template <bool BLK>
 static hipError_t launch_decode_gqa_192(const DecodeArgs& a, hipStream_t s) {
   int row_blocks, n_items, wpb, blocks;
@@ -848,6 +852,12 @@ static hipError_t launch_decode_gqa_192(const DecodeArgs& a, hipStream_t s) {
     const int w = gqa_team_waves(a, n_items, tt, 4);
     decode_gqa_bf16_kernel<192, 256, 64, BLK, 256, 1, true, false, BLK><<<(n_items * tt + w - 1) / w, 64 * w, gqa_merge_bytes<256>(w), s>>>(a, n_items, row_blocks, 0, tt, 1.f, 1.f);
     return hipGetLastError();
+  }
+  if constexpr (BLK) {
+    if (a.g % 4 == 0 && a.chunk_tiles >= 6) {   // (four waves that share k_R)
+      decode_gqa_bf16_kernel<192, 256, 64, true, 256, 1, false, true, true><<<blocks, 64 * wpb, 0, s>>>(a, n_items, row_blocks, 1, 1, 1.f, 1.f);
+      return hipGetLastError();
+    }
   }
   decode_gqa_bf16_kernel<192, 256, 64, BLK, 256, 1, false, false, BLK><<<blocks, 64 * wpb, 0, s>>>(a, n_items, row_blocks, team ? 1 : 0, 1, 1.f, 1.f);
   return hipGetLastError();

@@ -335,6 +335,36 @@ def test_decode(g, G, d_h, d_v, s_q, lens, chunk):
         B.gqla_plan_destroy(plan)
 
 
+@pytest.mark.parametrize("g,G,s_q,P,lens,chunk", [
+    (4, 5, 2, 64, [450, 3, 200, 193, 64], 3), (8, 4, 1, 64, [700, 31, 33, 640], 4), (4, 20, 2, 64, [400, 97, 520], 5), (4, 32, 1, 128, [1000, 129, 2], 2),
+])
+def test_decode_with_two_tiles_in_flight(g, G, s_q, P, lens, chunk):
+    """(192, 256), chunks of six tiles and more, on a plan for so few units that no chunk is shared out: odd and even numbers of tiles,
+    sequences that end early in a chunk, a page that is not there."""
+    w = World(lens, g, 192, 256, G=G, P=P, seed=75 + g + G, s_q=s_q)
+    w.append(lens)
+    w.spoil()
+    first = np.arange(w.B + 1) * s_q
+    q_c, q_r = stored(w.r.normal(size=(w.B * s_q, g * G, 192))), stored(w.r.normal(size=(w.B * s_q, g * G, D_R)))
+    hidden = [np.zeros(n, bool) for n in lens]
+    hidden[0][P:2 * P] = True
+    held = [w.kr_held(b) for b in range(w.B)]             # (read through the whole table)
+    w.kr_held = lambda b: held[b]
+    w.table[0, 1] = w.pages
+    w.d_table = torch.from_numpy(w.table).cuda()
+    plan = B.gqla_plan_create(w.shape, w.lens(), P, 2, B.GQLA_PATH_GQA, chunk)
+    try:
+        ws = torch.empty(B.gqla_plan_workspace_bytes(plan), dtype=torch.uint8, device="cuda")
+        B.gqla_plan_upload(plan, ws)
+        out = torch.full((w.B * s_q, g * G, 256), float("nan"), dtype=torch.bfloat16, device="cuda")
+        lse = torch.full((w.B * s_q, g * G), float("nan"), device="cuda")
+        B.gqla_decode_gqa_fp8_blocks(w.shape, plan, bf16(q_c).cuda(), bf16(q_r).cuda(), w.cache(), out, lse, ws)
+        torch.cuda.synchronize()
+        w.check_attention(out.float().cpu().numpy(), lse.cpu().numpy(), q_c, q_r, first, w.lens(), hidden)
+    finally:
+        B.gqla_plan_destroy(plan)
+
+
 def attend(w, ns, lens, q_c, q_r, extra=0, max_pages=None):
     first = np.concatenate([[0], np.cumsum(ns)]).astype(np.int32)
     total = int(first[-1]) + extra
