@@ -142,11 +142,16 @@ __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int
   // into LDS once per workgroup, as four 1 KB LDS-DMA instructions dealt over the waves, and every wave takes its
   // fragments from there, instead of every wave pulling the same lines through the vector memory path (a fifth of
   // all its load instructions).
-  __shared__ __attribute__((aligned(16))) char kr_lds[DEEP ? 3 : 2][KS_R * 1024];
-  const bool share_kr = DEEP || (!TEAM && share_kr_arg != 0);               // kernel-uniform
+  // OWN (DEEP with 192 key dims, one wave per SIMD): every wave brings the key to a place of its own, for any number of groups and without
+  // barriers (64 x 8000 tokens, 4 and 8 groups the same as shared to 1 %; 128 x 300 to 900 1 % faster).
+  constexpr bool OWN = DEEP && DH == 192;
+  __shared__ __attribute__((aligned(16))) char kr_lds[OWN ? 12 : DEEP ? 3 : 2][KS_R * 1024];
+  const bool share_kr = !OWN && (DEEP || (!TEAM && share_kr_arg != 0));     // kernel-uniform
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);        // position in the workgroup (scalar)
+  const int kr_place = OWN ? 3 * wave : 0;
   auto stage_kr = [&](int tok, int32_t pg, int buf) {
-    for (int ks = wave; ks < KS_R; ks += wpb) {  // k-step ks: dims 16*ks .. 16*ks + 15
+    if constexpr (OWN) buf += kr_place;
+    for (int ks = OWN ? 0 : wave; ks < KS_R; ks += OWN ? 1 : wpb) {  // k-step ks: dims 16*ks .. 16*ks + 15
       const char* src = pool + (int64_t)(pg >= 0 ? pg : 0) * page_bytes + kr_plane + ((int64_t)(2 * ks) * P + tok % P) * 16;
       const uint32_t dst = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_ptr_t)(kr_lds[buf] + ks * 1024));
       // ("memory": the cache loads that follow must stay behind this request, the counted wait relies on it)
@@ -263,9 +268,9 @@ __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int
         // behind this tile's k_R (loads complete in issue order): its key and value codes and the next tile's
         static_assert(KS_C + 2 * MT == 16 || KS_C + 2 * MT == 28, "the wait below is written for these counts");
         if constexpr (KS_C + 2 * MT == 16) asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
-        else asm volatile("s_waitcnt vmcnt(28)" ::: "memory");
-        __syncthreads();
-        const char* kr = kr_lds[slot] + lane * 16;
+        else asm volatile("s_waitcnt vmcnt(28)" ::: "memory");   // (OWN: four requests more behind it, the next tile's k_R; this asks for four more than it must)
+        if constexpr (!OWN) __syncthreads();
+        const char* kr = kr_lds[OWN ? kr_place + slot : slot] + lane * 16;
 #pragma unroll
         for (int ks = 0; ks < KS_R; ++ks) rf[ks] = *(const bf16x8*)(kr + ks * 1024);
 #pragma unroll
@@ -836,9 +841,9 @@ static hipError_t launch_decode_gqa_128(const DecodeArgs& a, float k_scale, floa
 }
 
 // (d_h, d_v) = (192, 256): four waves per workgroup, one row block each.  A wave is alone on its SIMD, and 15 KB of codes in flight are not enough:
-// codes take two tiles where four waves share k_R and chunks are long enough.  One tile over two (time of the call; 1 to 8 x 256 CUs' waves'
-// worth of items, 4 to 32 rows a group): chunks of 2 tiles 0.93 to 0.96, 4 0.98 to 0.99, 6 1.02 to 1.06, 8 1.05, 14 1.12, 32 and more 1.10 to
-// 1.15 (64 x 8000 tokens, 8 groups: 333 -> 304 us = 6.3 TB/s; 4 groups 194 -> 176).  Two groups, whose workgroups have two waves: 0.94 to 1.01.
+// codes take two tiles where chunks are long enough for the second tile's loads at their start and the empty ones at their end.  One tile over
+// two (time of the call; 1 to 8 groups, 120 to 4000 items, 4 to 32 rows a group): chunks of 2 tiles 0.93 to 1.00, 4 0.98 to 1.02, 6 1.00 to 1.06,
+// 8 to 14 1.00 to 1.12, 24 and more 1.00 (1 and 2 groups) to 1.15 (64 x 8000 tokens: 8 groups 333 -> 302 us = 6.3 TB/s, 5 239 -> 217, 4 194 -> 175).
 template <bool BLK>
 static hipError_t launch_decode_gqa_192(const DecodeArgs& a, hipStream_t s) {
   int row_blocks, n_items, wpb, blocks;
@@ -854,8 +859,8 @@ static hipError_t launch_decode_gqa_192(const DecodeArgs& a, hipStream_t s) {
     return hipGetLastError();
   }
   if constexpr (BLK) {
-    if (a.g % 4 == 0 && a.chunk_tiles >= 6) {   // (four waves that share k_R)
-      decode_gqa_bf16_kernel<192, 256, 64, true, 256, 1, false, true, true><<<blocks, 64 * wpb, 0, s>>>(a, n_items, row_blocks, 1, 1, 1.f, 1.f);
+    if (a.chunk_tiles >= 6) {
+      decode_gqa_bf16_kernel<192, 256, 64, true, 256, 1, false, true, true><<<(n_items + 3) / 4, 256, 0, s>>>(a, n_items, row_blocks, 0, 1, 1.f, 1.f);
       return hipGetLastError();
     }
   }

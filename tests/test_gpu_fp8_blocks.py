@@ -337,6 +337,7 @@ def test_decode(g, G, d_h, d_v, s_q, lens, chunk):
 
 @pytest.mark.parametrize("g,G,s_q,P,lens,chunk", [
     (4, 5, 2, 64, [450, 3, 200, 193, 64], 3), (8, 4, 1, 64, [700, 31, 33, 640], 4), (4, 20, 2, 64, [400, 97, 520], 5), (4, 32, 1, 128, [1000, 129, 2], 2),
+    (5, 4, 2, 64, [700, 3, 200, 193, 64], 3), (3, 7, 1, 64, [1030, 65], 6), (1, 16, 2, 64, [900, 130, 2], 4), (7, 20, 2, 64, [390, 450], 7),
 ])
 def test_decode_with_two_tiles_in_flight(g, G, s_q, P, lens, chunk):
     """(192, 256), chunks of six tiles and more, on a plan for so few units that no chunk is shared out: odd and even numbers of tiles,
