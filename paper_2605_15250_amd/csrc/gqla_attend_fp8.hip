@@ -431,9 +431,11 @@ hipError_t launch_attend(const AttendArgs& a, hipStream_t s) {
   attend_kernel<DH, DV><<<(unsigned)((spread ? (units + 7) / 8 * 8 : units) * a.g), 64 * kWaves, AttendTile<DH, DV>::kLds, s>>>(a, (int)tiles, spread);
   e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
+  // slices until there are 1024 workgroups (4 chunks of 100 to 512 tokens x 20 heads, two ranges: 67 -> 65 us against a slice per range)
+  constexpr int kGroups = 256 / (DV / 4);
   int slices = 1;
-  while (2 * slices <= a.splits && 2 * slices <= 256 / (DV / 4)) slices *= 2;
-  const int per = 256 / (DV / 4) / slices;
+  while (2 * slices <= a.splits && 2 * slices <= kGroups && (int64_t)a.total * a.h_q * slices < 1024 * kGroups) slices *= 2;
+  const int per = kGroups / slices;
   attend_merge_kernel<DV><<<(unsigned)(((int64_t)a.total * a.h_q + per - 1) / per), 256, 0, s>>>(a, slices);
   return hipGetLastError();
 }

@@ -456,7 +456,8 @@ def test_attend_rows_that_see_nothing_and_missing_pages():
     assert np.all(out[:5] == 0) and np.all(np.isneginf(lse[:5])) and np.all(out[48:48 + 64] == 0)
 
 
-@pytest.mark.parametrize("g,G,d_h,d_v,lens,ns", [(2, 4, 128, 128, [3000, 40], [3, 2]), (4, 5, 192, 256, [1500], [20]), (1, 1, 128, 128, [5000], [1])])
+@pytest.mark.parametrize("g,G,d_h,d_v,lens,ns", [(2, 4, 128, 128, [3000, 40], [3, 2]), (4, 5, 192, 256, [1500], [20]), (1, 1, 128, 128, [5000], [1]),
+                                                  (5, 4, 192, 256, [1500], [250]), (4, 8, 128, 128, [1100], [300])])
 def test_attend_splits_a_long_context(g, G, d_h, d_v, lens, ns):
     w = World(lens, g, d_h, d_v, G=G, P=256, seed=101 + g)
     w.append(lens)
