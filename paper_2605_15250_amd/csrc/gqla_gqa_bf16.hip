@@ -844,6 +844,7 @@ static hipError_t launch_decode_gqa_128(const DecodeArgs& a, float k_scale, floa
 // codes take two tiles where chunks are long enough for the second tile's loads at their start and the empty ones at their end.  One tile over
 // two (time of the call; 1 to 8 groups, 120 to 4000 items, 4 to 32 rows a group): chunks of 2 tiles 0.93 to 1.00, 4 0.98 to 1.02, 6 1.00 to 1.06,
 // 8 to 14 1.00 to 1.12, 24 and more 1.00 (1 and 2 groups) to 1.15 (64 x 8000 tokens: 8 groups 333 -> 302 us = 6.3 TB/s, 5 239 -> 217, 4 194 -> 175).
+// Teams, which have one to eight tiles a wave, keep one: 0.93 to 1.00.
 template <bool BLK>
 static hipError_t launch_decode_gqa_192(const DecodeArgs& a, hipStream_t s) {
   int row_blocks, n_items, wpb, blocks;
