@@ -4,8 +4,10 @@
 // wave (or 64, where 128 leave too few workgroups), and walks the tokens they see in stages of 64, which LDS-DMA brings into a ring of
 // buffers ahead of their use:
 //   S^T[token][row] = K Q^T,   O^T[dim][row] += V^T P^T
-// with one query row per lane throughout, a running maximum (moved only when outgrown) and an fp32 sum.
-// Codes are widened to bf16 with their block's power of two, exactly, right before their products; probabilities are rounded to bf16.
+// with one query row per lane throughout, a running maximum (moved only when outgrown) and fp32 sums.
+// Codes are widened to bf16 with their block's power of two, exactly, right before their products; probabilities are rounded to bf16, up to
+// 2^-8 of each.  The output's denominator sums them as rounded: a token that dominates a row then carries its rounding on both sides (with the
+// maximum lagging by up to 2^8 its probability is not 1).  The log-sum-exp takes the sum ahead of the rounding, as exact as fp32 has it.
 // (The 8-bit matrix instruction takes key codes as they are, with the queries as the sum of two E4M3 terms: two prompts of 2500 to 4000 tokens x
 // 128 heads then take 1042 us instead of 1107.  But it aligns the products of a sum to 2^-14 of the largest, where those in bf16 are
 // summed in fp32: logits were 3e-4 off.)
@@ -43,7 +45,7 @@ struct AttendTile {
   static constexpr int KC = DH / 32, KR = 4, MT = DV / 32;             // 1 KB pieces per 32 tokens: K codes, k_R, V codes
   static constexpr int kPieces = 2 * (KC + KR + MT), kPer = kPieces / kWaves;
   static constexpr int kPitch = DV * 2 + 16;                           // of an output row on its way through LDS
-  static constexpr int kState = MT * 4096 + 512;                       // a wave's O^T, maxima and sums on their way to another wave
+  static constexpr int kState = MT * 4096 + 768;                       // a wave's O^T, maxima and both sums on their way to another wave
   // Workgroups of a compute unit: registers allow three (two with value dims of 256), and two stages in the ring leave LDS for them.
   // (Three stages and two workgroups: a few rows over 20000 to 32000 tokens 41 us as well, 64 sequences of 2500 to 5000 158 us instead of 125.)
   static constexpr int kPerUnit = DV == 128 ? 3 : 2;
@@ -176,7 +178,7 @@ __global__ void __launch_bounds__(64 * kWaves, (AttendTile<DH, DV>::kPerUnit)) a
   for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[mt][i] = 0.f;
-  float m_run = GQLA_NEG_INF, l_run = 0.f;
+  float m_run = GQLA_NEG_INF, l_run = 0.f, d_run = 0.f;                // l, d: sums of the probabilities as they are, as rounded
   const int key_lane = (32 * h + (n & 19) + ((n & 4) << 1) + ((n & 8) >> 1)) * 16;
 
   // 32 tokens from `tok` on, whose pieces begin at lds (k_R and V behind the K pieces of both tiles).  Lane n takes the keys of token
@@ -207,6 +209,7 @@ __global__ void __launch_bounds__(64 * kWaves, (AttendTile<DH, DV>::kPerUnit)) a
       const float alpha = fast_exp2(m_run - (m_new == GQLA_NEG_INF ? 0.f : m_new));
       m_run = m_new;
       l_run *= alpha;
+      d_run *= alpha;
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -220,12 +223,16 @@ __global__ void __launch_bounds__(64 * kWaves, (AttendTile<DH, DV>::kPerUnit)) a
     for (int i = 0; i < 16; ++i) sum += p[i];
     l_run += sum;
     bf16x8 pf[2];
+    sum = 0.f;
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk) {
       const u32x4 w = {pack_bf16(p[8 * kk], p[8 * kk + 1]), pack_bf16(p[8 * kk + 2], p[8 * kk + 3]),
                        pack_bf16(p[8 * kk + 4], p[8 * kk + 5]), pack_bf16(p[8 * kk + 6], p[8 * kk + 7])};
       pf[kk] = __builtin_bit_cast(bf16x8, w);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) sum = add_bf16_pair(w[k], sum);
     }
+    d_run += sum;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       const u32x4 v8 = *(const u32x4*)(v_lds + mt * 1024);
@@ -276,6 +283,7 @@ __global__ void __launch_bounds__(64 * kWaves, (AttendTile<DH, DV>::kPerUnit)) a
         for (int q = 0; q < 4; ++q) *(f32x4*)(state + ((mt * 4 + q) * 64 + lane) * 16) = f32x4{o[mt][4 * q], o[mt][4 * q + 1], o[mt][4 * q + 2], o[mt][4 * q + 3]};
       *(float*)(state + MT * 4096 + lane * 4) = m_run;
       *(float*)(state + MT * 4096 + 256 + lane * 4) = l_run;
+      *(float*)(state + MT * 4096 + 512 + lane * 4) = d_run;
     }
     __syncthreads();
     if (team < half) {
@@ -284,6 +292,7 @@ __global__ void __launch_bounds__(64 * kWaves, (AttendTile<DH, DV>::kPerUnit)) a
       const float mine = fast_exp2(m_run - m_use), other = fast_exp2(m_other - m_use);
       m_run = m_new;
       l_run = l_run * mine + l_other * other;
+      d_run = d_run * mine + *(const float*)(state + MT * 4096 + 512 + lane * 4) * other;
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -295,8 +304,8 @@ __global__ void __launch_bounds__(64 * kWaves, (AttendTile<DH, DV>::kPerUnit)) a
     }
   }
 
-  const float l = pair_sum(l_run);
-  const float inv = l == 0.f ? 0.f : 1.f / l;                          // 0: nothing visible
+  const float l = pair_sum(l_run), d = pair_sum(d_run);
+  const float inv = d == 0.f ? 0.f : 1.f / d;                          // 0: nothing visible
   const float lse = l == 0.f ? GQLA_NEG_INF : (m_run + fast_log2(l)) * kLn2;
   const bool row_ok = rho0 + n <= last;
   const int64_t at = row * a.h_q + head;

@@ -47,9 +47,9 @@ __device__ __forceinline__ bf16x8 widen_e4m3(uint32_t w0, uint32_t w1, float sca
 // through LDS, so that one partial per item reaches memory.
 // DEEP (8-bit codes, RB = 1, no teams, shared k_R): the codes of two tiles in registers, see the loop.
 // BLK (8-bit codes): a power of two per (32 tokens, group) for K and for V instead of k_scale and v_scale.  A tile's pair comes
-// through the scalar cache with the request of its codes and enters where they are widened, at no instruction.  The
-// denominator sums the probabilities ahead of their rounding to bf16 (which saves unpacking them: 2^-9 of each, at random, stays in the
-// output, and the log-sum-exp is as exact as fp32 has it).  64 sequences of 8192 tokens x 128 heads, two rows: 172 us = 6.7 TB/s, as
+// through the scalar cache with the request of its codes and enters where they are widened, at no instruction.  Two sums of the
+// probabilities: as rounded to bf16 for the output's denominator, which numerator and denominator then share (below), and ahead of
+// that rounding for the log-sum-exp, which is as exact as fp32 has it.  64 sequences of 8192 tokens x 128 heads, two rows: 172 us = 6.7 TB/s, as
 // with one scale (170); one sequence of 1000 tokens x 32 heads 6.7 us.
 template <int DH, int DV, int DR, bool FP8, int MAXT, int RB, bool TEAM, bool DEEP, bool BLK = false>
 __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int n_items, int row_blocks, int share_kr_arg,
@@ -213,11 +213,12 @@ __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int
   };
 
   f32x16 o[RB][MT];
-  float m_run[RB], l_run[RB];
+  float m_run[RB], l_run[RB], d_run[BLK ? RB : 1];   // l: sum of the probabilities; BLK: of the unrounded ones, d of the rounded ones
 #pragma unroll
   for (int x = 0; x < RB; ++x) {
     m_run[x] = GQLA_NEG_INF;
     l_run[x] = 0.f;
+    if constexpr (BLK) d_run[x] = 0.f;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -310,6 +311,7 @@ __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int
           const float alpha = fast_exp2(m_run[0] - ((m_new == GQLA_NEG_INF) ? 0.f : m_new));
           m_run[0] = m_new;
           l_run[0] *= alpha;
+          if constexpr (BLK) d_run[0] *= alpha;
 #pragma unroll
           for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -319,7 +321,7 @@ __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int
 #pragma unroll
         for (int i = 0; i < 16; ++i) sv[i] = fast_exp2(sv[i] - m_use);
         bf16x8 pf[2];
-        float psum = 0.f;
+        float psum = 0.f, dsum = 0.f;
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
           const uint32_t x0 = pack_bf16(sv[8 * kk + 0], sv[8 * kk + 1]), x1 = pack_bf16(sv[8 * kk + 2], sv[8 * kk + 3]);
@@ -327,6 +329,8 @@ __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int
           if constexpr (BLK) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) psum += sv[8 * kk + i];
+#pragma unroll
+            for (uint32_t wd : {x0, x1, y0, y1}) dsum = add_bf16_pair(wd, dsum);
           } else {
 #pragma unroll
             for (uint32_t wd : {x0, x1, y0, y1}) psum += __builtin_bit_cast(float, wd << 16) + __builtin_bit_cast(float, wd & 0xffff0000u);
@@ -342,6 +346,7 @@ __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int
           pf[kk] = __builtin_bit_cast(bf16x8, w);
         }
         l_run[0] += psum;
+        if constexpr (BLK) d_run[0] += dsum;
         // values of tokens outside the chunk may hold any code (NaN included): code 0 is 0
         if (tok + 32 > ce.tok_end || !tile_ok) {
           const int lim = tile_ok ? ce.tok_end : 0;
@@ -500,6 +505,7 @@ __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int
           const float alpha = fast_exp2(m_run[x] - ((m_new == GQLA_NEG_INF) ? 0.f : m_new));
           m_run[x] = m_new;
           l_run[x] *= alpha;
+          if constexpr (BLK) d_run[x] *= alpha;
 #pragma unroll
           for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -512,7 +518,7 @@ __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int
         // P^T fragments: k-step kk covers tokens tok + 16*kk .. +15, lane half h needs tokens 8h .. 8h+7 of them.
         // The denominator sums the probabilities as the matrix cores see them (rounded to bf16): numerator and
         // denominator then weigh every token alike, whatever the reference of the exponentials is.
-        float psum = 0.f;
+        float psum = 0.f, dsum = 0.f;
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
           const uint32_t x0 = pack_bf16(sv[8 * kk + 0], sv[8 * kk + 1]), x1 = pack_bf16(sv[8 * kk + 2], sv[8 * kk + 3]);
@@ -520,6 +526,8 @@ __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int
           if constexpr (BLK) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) psum += sv[8 * kk + i];
+#pragma unroll
+            for (uint32_t wd : {x0, x1, y0, y1}) dsum = add_bf16_pair(wd, dsum);
           } else {
 #pragma unroll
             for (uint32_t wd : {x0, x1, y0, y1}) psum += __builtin_bit_cast(float, wd << 16) + __builtin_bit_cast(float, wd & 0xffff0000u);
@@ -535,6 +543,7 @@ __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int
           pf[x][kk] = __builtin_bit_cast(bf16x8, w);
         }
         l_run[x] += psum;  // per-lane partial sum; the two half-waves are added at the end
+        if constexpr (BLK) d_run[x] += dsum;
       }
 
       // values of tokens outside the chunk may hold any bits (NaN included): zero them so that 0 * v stays 0
@@ -562,10 +571,10 @@ __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int
 
   if constexpr (TEAM) {
     // ---- merge of the team's partial states (row = lane % 32) ----
-    // dyn_lds: O^T of every wave as [wave][quad q = 4 mt + i/4][lane][4] fp32 (MT * 4 KB per wave), then m and l per (wave,
+    // dyn_lds: O^T of every wave as [wave][quad q = 4 mt + i/4][lane][4] fp32 (MT * 4 KB per wave), then m and l (BLK: and d) per (wave,
     // row).  Wave w of a team sums quads kQuads / tt * w, ... of all its waves in a fixed order and writes them.
     constexpr int kQuads = MT * 4, kMaxTeam = MAXT / 64;
-    float* const ml_lds = (float*)dyn_lds + wpb * kQuads * 64 * 4 + (wave_in_wg - tw) * 32;   // l: 32 wpb floats further
+    float* const ml_lds = (float*)dyn_lds + wpb * kQuads * 64 * 4 + (wave_in_wg - tw) * 32;   // l: 32 wpb floats further, d: as many again
     float* const o_lds = (float*)dyn_lds + (wave_in_wg - tw) * kQuads * 64 * 4;
     const float l_mine = pair_sum(l_run[0]);
 #pragma unroll
@@ -578,21 +587,27 @@ __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int
       ml_lds[tw * 32 + n] = m_run[0];
       ml_lds[(wpb + tw) * 32 + n] = l_mine;
     }
+    if constexpr (BLK) {
+      const float d_mine = pair_sum(d_run[0]);
+      if (h == 0) ml_lds[(2 * wpb + tw) * 32 + n] = d_mine;
+    }
     __syncthreads();
     float m_all = GQLA_NEG_INF;
     for (int w = 0; w < tt; ++w) m_all = fmaxf(m_all, ml_lds[w * 32 + n]);
     const float m_use = (m_all == GQLA_NEG_INF) ? 0.f : m_all;
-    float c[kMaxTeam], l_all = 0.f;
+    float c[kMaxTeam], l_all = 0.f, d_all = 0.f;
 #pragma unroll
     for (int w = 0; w < kMaxTeam; ++w) {
       c[w] = 0.f;
       if (w < tt) {
         c[w] = fast_exp2(ml_lds[w * 32 + n] - m_use);  // 0 for a wave that saw no visible token
         l_all += c[w] * ml_lds[(wpb + w) * 32 + n];
+        if constexpr (BLK) d_all += c[w] * ml_lds[(2 * wpb + w) * 32 + n];
       }
     }
     const bool ok = row_ok[0];
-    const float inv = (l_all > 0.f ? 1.f / l_all : 0.f) * (FP8 && !BLK ? v_scale : 1.f);
+    if constexpr (!BLK) d_all = l_all;
+    const float inv = (d_all > 0.f ? 1.f / d_all : 0.f) * (FP8 && !BLK ? v_scale : 1.f);
     const int rho = t_of[0] * a.h_q + head_of[0];
     const int64_t prow = (int64_t)chunk * a.M + rho;
     // chunk partial in fp32, 4-dim vectors ordered [chunk][32-row block][d_v / 4][row] (part_vec_index): this lane
@@ -620,8 +635,10 @@ __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int
 #pragma unroll
   for (int x = 0; x < RB; ++x) {
     const float l_tot = pair_sum(l_run[x]);
+    float d_tot = l_tot;
+    if constexpr (BLK) d_tot = pair_sum(d_run[x]);
     if (!row_ok[x]) continue;
-    const float inv = (l_tot > 0.f ? 1.f / l_tot : 0.f) * (FP8 && !BLK ? v_scale : 1.f);
+    const float inv = (d_tot > 0.f ? 1.f / d_tot : 0.f) * (FP8 && !BLK ? v_scale : 1.f);
     const int rho = t_of[x] * a.h_q + head_of[x];
     const int64_t prow = (int64_t)chunk * a.M + rho;
     // chunk partial in fp32, 4-dim vectors ordered [chunk][32-row block][d_v / 4][row] (part_vec_index): consecutive rows
@@ -791,8 +808,8 @@ static int gqa_team_waves(const DecodeArgs& a, int n_items, int tt, int waves) {
   while (w < waves && ((int64_t)n_items * tt + w - 1) / w > a.num_cus) w *= 2;
   return w;
 }
-template <int DV>
-constexpr int gqa_merge_bytes(int waves) { return waves * (DV / 32 * 4 * 64 * 16 + 2 * 32 * 4); }  // O^T, then m and l per (wave, row)
+template <int DV, bool BLK>
+constexpr int gqa_merge_bytes(int waves) { return waves * (DV / 32 * 4 * 64 * 16 + (BLK ? 3 : 2) * 32 * 4); }  // O^T, then m, l (and d) per (wave, row)
 
 // 8-bit codes, eight waves that share k_R: two tiles of codes in flight where a chunk is long enough for the second tile's loads
 // at its start and the two empty tiles at its end; the more query rows, the later.  One tile over two (time of the call), 8 groups,
@@ -823,10 +840,10 @@ static hipError_t launch_decode_gqa_128(const DecodeArgs& a, float k_scale, floa
   const int tt = a.g == 1 ? 8 : gqa_token_team_size(a, n_items, 8);
   if (tt > 1) {
     static const hipError_t attr = hipFuncSetAttribute((const void*)decode_gqa_bf16_kernel<128, 128, 64, FP8, 512, 1, true, false, BLK>,
-                                                       hipFuncAttributeMaxDynamicSharedMemorySize, gqa_merge_bytes<128>(8));
+                                                       hipFuncAttributeMaxDynamicSharedMemorySize, gqa_merge_bytes<128, BLK>(8));
     if (attr != hipSuccess) return attr;
     const int w = gqa_team_waves(a, n_items, tt, 8);
-    decode_gqa_bf16_kernel<128, 128, 64, FP8, 512, 1, true, false, BLK><<<(n_items * tt + w - 1) / w, 64 * w, gqa_merge_bytes<128>(w), s>>>(a, n_items, row_blocks, 0, tt,
+    decode_gqa_bf16_kernel<128, 128, 64, FP8, 512, 1, true, false, BLK><<<(n_items * tt + w - 1) / w, 64 * w, gqa_merge_bytes<128, BLK>(w), s>>>(a, n_items, row_blocks, 0, tt,
                                                                                                                          k_scale, v_scale);
     return hipGetLastError();
   }
@@ -853,10 +870,10 @@ static hipError_t launch_decode_gqa_192(const DecodeArgs& a, hipStream_t s) {
   const int tt = gqa_token_team_size(a, n_items, 4);
   if (tt > 1) {
     static const hipError_t attr = hipFuncSetAttribute((const void*)decode_gqa_bf16_kernel<192, 256, 64, BLK, 256, 1, true, false, BLK>,
-                                                       hipFuncAttributeMaxDynamicSharedMemorySize, gqa_merge_bytes<256>(4));
+                                                       hipFuncAttributeMaxDynamicSharedMemorySize, gqa_merge_bytes<256, BLK>(4));
     if (attr != hipSuccess) return attr;
     const int w = gqa_team_waves(a, n_items, tt, 4);
-    decode_gqa_bf16_kernel<192, 256, 64, BLK, 256, 1, true, false, BLK><<<(n_items * tt + w - 1) / w, 64 * w, gqa_merge_bytes<256>(w), s>>>(a, n_items, row_blocks, 0, tt, 1.f, 1.f);
+    decode_gqa_bf16_kernel<192, 256, 64, BLK, 256, 1, true, false, BLK><<<(n_items * tt + w - 1) / w, 64 * w, gqa_merge_bytes<256, BLK>(w), s>>>(a, n_items, row_blocks, 0, tt, 1.f, 1.f);
     return hipGetLastError();
   }
   if constexpr (BLK) {
