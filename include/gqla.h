@@ -335,7 +335,9 @@ int64_t gqla_expanded_fp8_bytes_per_token(int32_t groups, int32_t d_h, int32_t d
  * expanded->seq_lens on the device) into one with block scales, same page geometry; bytes of slots no token owns and scales
  * of blocks no token owns are left as they are.  Errors as for gqla_quantize_expanded.
  *
- * gqla_decode_gqa_fp8_blocks is gqla_decode_gqa over such a cache: same plan, workspace, outputs and errors. */
+ * gqla_decode_gqa_fp8_blocks is gqla_decode_gqa over such a cache: same plan, workspace, outputs and errors.  A NaN among the keys that a
+ * row sees makes the row and its lse NaN, one among the values its own dim (with two step tokens a NaN value of the second one's reaches
+ * the first row as well). */
 gqla_status gqla_quantize_expanded_fp8_blocks(const gqla_shape* shape, const gqla_cache* expanded, const gqla_cache* expanded_blocks,
                                               void* stream);
 gqla_status gqla_decode_gqa_fp8_blocks(const gqla_shape* shape, const gqla_plan* plan, const void* q_c, const void* q_r,

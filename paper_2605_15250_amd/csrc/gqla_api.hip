@@ -247,6 +247,7 @@ CombineArgs combine_args(const gqla_shape* s, const gqla_plan* plan, void* ws, c
   c.s_q = s->s_q;
   c.M = s->s_q * s->h_q;
   c.n_chunks = (int32_t)plan->chunks.size();
+  c.nan_stays = false;
   return c;
 }
 
@@ -859,6 +860,7 @@ gqla_status gqla_decode_gqa_fp8_blocks(const gqla_shape* shape, const gqla_plan*
   const DecodeArgs a = decode_args(shape, plan, q_c, q_r, expanded_blocks, ws);
   CombineArgs c = combine_args(shape, plan, ws, nullptr, out, lse);
   c.d_h = value_dim(shape);  // partials and outputs are value dims
+  c.nan_stays = true;
   const KernelTimer timer(s);
   hipError_t e = timer.begin();
   if (e == hipSuccess) e = launch_decode_gqa_fp8_blocks(a, s);

@@ -596,18 +596,24 @@ __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int
     for (int w = 0; w < tt; ++w) m_all = fmaxf(m_all, ml_lds[w * 32 + n]);
     const float m_use = (m_all == GQLA_NEG_INF) ? 0.f : m_all;
     float c[kMaxTeam], l_all = 0.f, d_all = 0.f;
+    uint32_t saw = 0;                                // BLK: waves with a token that the row sees
 #pragma unroll
     for (int w = 0; w < kMaxTeam; ++w) {
       c[w] = 0.f;
       if (w < tt) {
         c[w] = fast_exp2(ml_lds[w * 32 + n] - m_use);  // 0 for a wave that saw no visible token
         l_all += c[w] * ml_lds[(wpb + w) * 32 + n];
-        if constexpr (BLK) d_all += c[w] * ml_lds[(2 * wpb + w) * 32 + n];
+        if constexpr (BLK) {
+          const float d_w = ml_lds[(2 * wpb + w) * 32 + n];
+          d_all += c[w] * d_w;
+          saw |= (uint32_t)(d_w != 0.f) << w;
+        }
       }
     }
     const bool ok = row_ok[0];
     if constexpr (!BLK) d_all = l_all;
-    const float inv = (d_all > 0.f ? 1.f / d_all : 0.f) * (FP8 && !BLK ? v_scale : 1.f);
+    const bool sees = BLK ? d_all != 0.f : d_all > 0.f;   // (BLK: a NaN among the visible keys stays one)
+    const float inv = (sees ? 1.f / d_all : 0.f) * (FP8 && !BLK ? v_scale : 1.f);
     const int rho = t_of[0] * a.h_q + head_of[0];
     const int64_t prow = (int64_t)chunk * a.M + rho;
     // chunk partial in fp32, 4-dim vectors ordered [chunk][32-row block][d_v / 4][row] (part_vec_index): this lane
@@ -623,12 +629,13 @@ __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int
       for (int w = 0; w < kMaxTeam; ++w) {
         if (w >= tt) break;
         const f32x4 v = *(const f32x4*)(o_lds + ((w * kQuads + quad) * 64 + lane) * 4);
-        if (c[w] > 0.f) acc += c[w] * v;  // (a wave without tiles holds zeros; one whose rows were all masked may hold anything times 0)
+        // (a wave without tiles holds zeros; one whose rows were all masked may hold anything times 0)
+        if (BLK ? saw >> w & 1 : c[w] > 0.f) acc += c[w] * v;
       }
       acc *= inv;
       if (ok) *(f32x4*)(po + 2 * quad * (32 * 4)) = acc;
     }
-    if (ok && tw == 0 && h == 0) a.part_lse[prow] = l_all > 0.f ? (m_all + fast_log2(l_all)) * kLn2 : GQLA_NEG_INF;
+    if (ok && tw == 0 && h == 0) a.part_lse[prow] = sees ? (m_all + fast_log2(l_all)) * kLn2 : GQLA_NEG_INF;
     return;
   }
 
@@ -638,7 +645,8 @@ __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int
     float d_tot = l_tot;
     if constexpr (BLK) d_tot = pair_sum(d_run[x]);
     if (!row_ok[x]) continue;
-    const float inv = (d_tot > 0.f ? 1.f / d_tot : 0.f) * (FP8 && !BLK ? v_scale : 1.f);
+    const bool sees = BLK ? d_tot != 0.f : d_tot > 0.f;   // (BLK: a NaN among the visible keys stays one)
+    const float inv = (sees ? 1.f / d_tot : 0.f) * (FP8 && !BLK ? v_scale : 1.f);
     const int rho = t_of[x] * a.h_q + head_of[x];
     const int64_t prow = (int64_t)chunk * a.M + rho;
     // chunk partial in fp32, 4-dim vectors ordered [chunk][32-row block][d_v / 4][row] (part_vec_index): consecutive rows
@@ -653,7 +661,7 @@ __global__ void __launch_bounds__(MAXT) decode_gqa_bf16_kernel(DecodeArgs a, int
       for (int q = 0; q < 4; ++q)
         *(f32x4*)(po + (8 * mt + 2 * q) * (32 * 4)) =
             f32x4{o[x][mt][4 * q] * inv, o[x][mt][4 * q + 1] * inv, o[x][mt][4 * q + 2] * inv, o[x][mt][4 * q + 3] * inv};
-    if (h == 0) a.part_lse[prow] = l_tot > 0.f ? (m_run[x] + fast_log2(l_tot)) * kLn2 : GQLA_NEG_INF;
+    if (h == 0) a.part_lse[prow] = sees ? (m_run[x] + fast_log2(l_tot)) * kLn2 : GQLA_NEG_INF;
   }
 }
 
@@ -718,7 +726,7 @@ __global__ void __launch_bounds__(256) combine_gqa_bf16_kernel(CombineArgs a) {
     for (int k = 0; k < kNB; ++k) {
       const float w = __expf(l[k] - m_use);
       den += w;
-      if (w > 0.f) {  // a chunk without visible tokens may hold anything
+      if (a.nan_stays ? l[k] != GQLA_NEG_INF : w > 0.f) {  // a chunk without visible tokens may hold anything
 #pragma unroll
         for (int v = 0; v < VPT; ++v) acc[v] += w * x[k][v];
       }
@@ -746,11 +754,11 @@ __global__ void __launch_bounds__(256) combine_gqa_bf16_kernel(CombineArgs a) {
         den += w * ml[1][c][n];
         sum += w * part[c][slot][n];
       }
-      const float inv = den > 0.f ? 1.f / den : 0.f;
+      const float inv = den > 0.f || a.nan_stays && den != 0.f ? 1.f / den : 0.f;
       *(u32x2*)(tile + n * PITCH + slot * 8) = u32x2{pack_bf16(sum[0] * inv, sum[1] * inv), pack_bf16(sum[2] * inv, sum[3] * inv)};
     }
   } else {
-    const float inv = den > 0.f ? 1.f / den : 0.f;
+    const float inv = den > 0.f || a.nan_stays && den != 0.f ? 1.f / den : 0.f;
 #pragma unroll
     for (int v = 0; v < VPT; ++v)
       *(u32x2*)(tile + n * PITCH + (vs + VS * v) * 8) = u32x2{pack_bf16(acc[v][0] * inv, acc[v][1] * inv), pack_bf16(acc[v][2] * inv, acc[v][3] * inv)};

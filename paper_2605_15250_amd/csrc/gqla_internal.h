@@ -48,6 +48,7 @@ struct CombineArgs {
   float* lse;                 // optional [B][s_q][h_q]
   int32_t B, h_q, g, G, d_h, r_kv, s_q, M;
   int32_t n_chunks;           // of the whole batch (launch-shape choices only)
+  bool nan_stays;             // GQA path, block scales: a chunk's NaN makes the row's; otherwise such a chunk counts as one without tokens
 };
 
 struct ExpandArgs {
