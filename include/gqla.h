@@ -386,7 +386,7 @@ gqla_status gqla_append_expanded_fp8_blocks(const gqla_shape* shape, const gqla_
  * [total][h_q][d_h] and q_r [total][h_q][d_r] (rotated), out [total][h_q][d_v], lse [total][h_q] fp32 or NULL.  Row i of a sequence
  * with n of them sits at position t = L_b - n + i (L_b from expanded_blocks->seq_lens on the device, new tokens included and already
  * appended) and sees tokens s <= t.  A row that sees nothing (t < 0, or only pages outside the pool) gets out = 0, lse = -inf; rows
- * that no sequence owns are not touched.  A NaN among the values of a tile of 32 tokens reaches every row that has a token of the tile in sight.
+ * that no sequence owns are not touched.  A NaN reaches the rows that see its token and no others: a value's its own dim, a key's the row and its lse.
  * ws: device scratch of at least gqla_attend_gqa_workspace_bytes(shape, first, total, expanded_blocks) bytes, 16-byte aligned (fp32
  * partial outputs over ranges of a long context, where there are few rows; may be NULL when that is 0).  It depends on the sizes
  * only, max_pages * page_size standing for the longest context, and holds nothing between calls; calls whose kernels can overlap

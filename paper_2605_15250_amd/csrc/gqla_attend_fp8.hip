@@ -37,6 +37,34 @@ __device__ __forceinline__ bf16x8 widen_codes(uint32_t w0, uint32_t w1, float sc
   return __builtin_bit_cast(bf16x8, r);
 }
 
+// NaN codes are 0x7f and 0xff: bit 7 of their bytes, and a word with 0 in their place.
+__device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+__device__ __forceinline__ uint32_t without_nans(uint32_t w) {
+  const uint32_t bits = nan_codes(w);
+  return w & ~(bits | (bits - (bits >> 7)));
+}
+// Which outputs of a 32x32 tile have a NaN in sight: the product of the indicators [code is NaN] and [row sees the token].  codes: value operand
+// of two k-steps (byte e: token 16 (e / 8) + 8 h + e % 8); limit: tokens of the tile that this lane's row sees.  0 or NaN per output.
+__device__ __forceinline__ f32x16 seen_nans(const u32x4& codes, int limit, int h) {
+  f32x16 r;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) r[i] = 0.f;
+#pragma unroll
+  for (int kk = 0; kk < 2; ++kk) {
+    u32x4 sees;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int t = 16 * kk + 8 * h + 2 * k;
+      sees[k] = (t < limit ? 0x3f80u : 0u) | (t + 1 < limit ? 0x3f800000u : 0u);
+    }
+    constexpr uint32_t kOne = 0x38;   // the code of 1
+    r = mfma32(widen_codes((nan_codes(codes[2 * kk]) >> 7) * kOne, (nan_codes(codes[2 * kk + 1]) >> 7) * kOne, 1.f), __builtin_bit_cast(bf16x8, sees), r);
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) r[i] = r[i] > 0.f ? __builtin_nanf("") : 0.f;
+  return r;
+}
+
 constexpr int kWaves = 4, kRows = 32 * kWaves, kStage = 64;
 constexpr float kRescale = 8.f;   // log2 units by which a maximum may outgrow the reference of the exponentials
 
@@ -178,6 +206,7 @@ __global__ void __launch_bounds__(64 * kWaves, (AttendTile<DH, DV>::kPerUnit)) a
   for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[mt][i] = 0.f;
+  bool had_nans = false;                                               // among values that only some of the wave's rows see
   float m_run = GQLA_NEG_INF, l_run = 0.f, d_run = 0.f;                // l, d: sums of the probabilities as they are, as rounded
   const int key_lane = (32 * h + (n & 19) + ((n & 4) << 1) + ((n & 8) >> 1)) * 16;
 
@@ -235,7 +264,21 @@ __global__ void __launch_bounds__(64 * kWaves, (AttendTile<DH, DV>::kPerUnit)) a
     d_run += sum;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
-      const u32x4 v8 = *(const u32x4*)(v_lds + mt * 1024);
+      u32x4 v8 = *(const u32x4*)(v_lds + mt * 1024);
+      if (tok + 32 > vis_min) {
+        // a weight of 0 does not keep a NaN away from a row (0 * NaN = NaN): they are taken out, and the rows that see them get them at the end
+        const uint32_t found = nan_codes(v8[0]) | nan_codes(v8[1]) | nan_codes(v8[2]) | nan_codes(v8[3]);
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(found != 0) != 0, 0)) {
+          uint32_t seen = 0;                                           // (slots that no row sees may hold anything)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int count = min(max(vis_max - tok - 16 * (k >> 1) - 8 * h - 4 * (k & 1), 0), 4);
+            seen |= nan_codes(v8[k]) & (uint32_t)((1ull << (8 * count)) - 1);
+            v8[k] = without_nans(v8[k]);
+          }
+          had_nans |= __builtin_amdgcn_ballot_w64(seen != 0) != 0;
+        }
+      }
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk) o[mt] = mfma32(widen_codes(v8[2 * kk], v8[2 * kk + 1], sc_v), pf[kk], o[mt]);
     }
@@ -252,17 +295,6 @@ __global__ void __launch_bounds__(64 * kWaves, (AttendTile<DH, DV>::kPerUnit)) a
     if (st + 1 < st1) sc = scales_of(here);
     if (st + 2 < st1) next = look_up();
     const int tok = st * kStage;
-    if (there && r.len - tok < kStage) {   // the sequence ends here: value codes behind it may be anything (NaN included), a weight of 0 is not enough
-      char* vectors = smem + (buf * PIECES + 2 * (KC + KR)) * 1024 + lane * 16;
-      for (int p = wave; p < 2 * MT; p += kWaves) {
-        u32x4 v = *(const u32x4*)(vectors + p * 1024);
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (tok + p / MT * 32 + 16 * (e >> 3) + 8 * h + (e & 7) >= r.len) v[e >> 2] &= ~(0xffu << (8 * (e & 3)));
-        *(u32x4*)(vectors + p * 1024) = v;
-      }
-      __syncthreads();
-    }
     if (there) {                                                       // a page that is not there holds nothing
       const char *ring = smem + buf * (PIECES * 1024), *keys = ring + key_lane, *vals = ring + 2 * (KC + KR) * 1024 + lane * 16;
       // tile q of 32 tokens is team q mod teams's
@@ -270,6 +302,14 @@ __global__ void __launch_bounds__(64 * kWaves, (AttendTile<DH, DV>::kPerUnit)) a
       if (tok < vis_max && team == first) attend_tile(tok, keys, keys + 2 * KC * 1024, vals, now[0], now[1]);
       if (tok + 32 < vis_max && team == (first + 1 & (teams - 1)))
         attend_tile(tok + 32, keys + KC * 1024, keys + (2 * KC + KR) * 1024, vals + MT * 1024, now[2], now[3]);
+    }
+  }
+  if (__builtin_expect(had_nans, 0)) {                                 // what was taken out: those tiles' values once more
+    for (int tok = max(vis_min & ~31, st0 * kStage); tok < min((int64_t)vis_max, (int64_t)st1 * kStage); tok += 32) {
+      const int32_t pg = page_of_uniform(a.cache, r.b, tok / P);
+      const char* codes = pool + (int64_t)max(pg, 0) * page_bytes + (uint32_t)(P * gc * DH + (j * (P / 32) + tok % P / 32) * DV * 32) + off_v;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) o[mt] += seen_nans(*(const u32x4*)(codes + mt * 1024), pg >= 0 ? vis - tok : 0, h);
     }
   }
   // the teams' states become one, half of them at a time

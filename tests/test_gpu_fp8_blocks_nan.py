@@ -58,6 +58,19 @@ def reference(w, q_c, q_r, first, lens):
 
 
 @pytest.mark.parametrize("g,G,d_h,d_v,lens,ns,at", [
+    (2, 4, 128, 128, [70, 40], [70, 11], [69, 39]), (2, 1, 128, 128, [64, 200], [64, 200], [40, 199]), (8, 16, 128, 128, [257], [130], [256]),
+    (1, 3, 128, 128, [300, 33], [150, 33], [170, 1]), (5, 4, 192, 256, [200, 90], [70, 90], [140, 89]), (4, 5, 192, 256, [130], [130], [97]),
+    (2, 4, 128, 128, [3000, 40], [3, 2], [2999, 39]), (5, 4, 192, 256, [1500], [250], [1300]),
+])
+def test_attention_with_a_value_that_only_some_rows_see(g, G, d_h, d_v, lens, ns, at):
+    bad = [(b, t, b % g, 5 + 64 * b) for b, t in enumerate(at)] + [(0, at[0], g - 1, d_v - 1)]
+    w = world(lens, g, G, d_h, d_v, 64, 1, 501 + g + G, bad_v=bad)
+    q_c, q_r = stored(w.r.normal(size=(sum(ns), g * G, d_h))), stored(w.r.normal(size=(sum(ns), g * G, D_R)))
+    out, lse, first, _ = attend(w, ns, lens, q_c, q_r)
+    check(w, out, lse, q_c, q_r, first, lens, bad_v=bad)
+
+
+@pytest.mark.parametrize("g,G,d_h,d_v,lens,ns,at", [
     (2, 4, 128, 128, [70, 40], [70, 11], [69, 3]), (4, 5, 192, 256, [130], [130], [97]), (2, 4, 128, 128, [3000, 40], [3, 2], [2999, 20]),
     (2, 4, 128, 128, [3000, 40], [3, 2], [700, 39]),
 ])
