@@ -39,6 +39,12 @@ def build_latent_pool(cfg, lens, table, num_pages, row_fn, fill=float("nan")) ->
     return pool
 
 
+def apart(x):
+    """x, or where its rows are not runs of adjacent elements (dims apart, one row expanded over all) a copy of it whose rows are."""
+    n = x.shape[0]
+    return x if n == 0 or x[0].is_contiguous() and (n == 1 or x.stride(0) >= x[0].numel()) else x.contiguous()
+
+
 class Decoder:
     """Holds the device-resident state of one configuration and runs the four entry points on it."""
 
@@ -232,8 +238,12 @@ class Decoder:
         return self.expanded_blocks_pool
 
     def append_expanded(self, rope_base, k_c, v, k_r, q_r=None, first=None, blocks=False):
-        """New rows k_c [n, groups * d_h], v [n, groups * d_v], k_r [n, d_r] (unit stride inside a row) into the expanded cache, or into the
-        one with block scales; returns the rotated queries.  first: device int32 [B + 1], None: s_q rows per sequence."""
+        """New rows k_c [n, groups * d_h], v [n, groups * d_v], k_r [n, d_r] into the expanded cache, or into the one with block scales;
+        returns the rotated queries of q_r [n, heads of the slice, d_r], contiguous.  Rows may lie apart, as the parts of a joint buffer do; q_r
+        with other strides than its own, and rows that are not runs of dims, are copied first.  first: device int32 [B + 1], None: s_q rows per
+        sequence."""
+        k_c, v, k_r = apart(k_c), apart(v), apart(k_r)
+        q_r = q_r.contiguous() if q_r is not None else None
         q_rot = torch.empty_like(q_r) if q_r is not None else None
         n = k_c.shape[0]
         rows = B.make_new_rows(k_c, v, k_r, q_r, q_rot, first, n, *(x.stride(0) if n > 1 else 0 for x in (k_c, v, k_r)))   # (one row: no stride)
