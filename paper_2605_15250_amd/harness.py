@@ -81,7 +81,6 @@ class Decoder:
         self.expanded_blocks_pool = None
         self.ws_e = None                                        # scratch of the expand call
         self.ws_o = None                                        # scratch of the output projection
-        self.ws_t = None                                        # scratch of the prompt chunks' attention
 
     def close(self):
         for p in (self.plan_a, self.plan_g):
@@ -273,9 +272,9 @@ class Decoder:
             lse = torch.empty((n, heads), dtype=torch.float32, device="cuda")
         cache = self.expanded_blocks_cache()
         nbytes = B.gqla_attend_gqa_workspace_bytes(self.shape_gqa, first, n, cache)
-        if nbytes and (self.ws_t is None or self.ws_t.numel() < nbytes):
-            self.ws_t = torch.empty((nbytes,), dtype=torch.uint8, device="cuda")
-        B.gqla_attend_gqa_fp8_blocks(self.shape_gqa, first, n, q_c, q_r, cache, out, lse, self.ws_t if nbytes else None)
+        # (one for each call: a recorded call keeps using its own, in the graph's memory, and calls on two streams overlap)
+        ws = torch.empty((nbytes,), dtype=torch.uint8, device="cuda") if nbytes else None
+        B.gqla_attend_gqa_fp8_blocks(self.shape_gqa, first, n, q_c, q_r, cache, out, lse, ws)
         return out, lse
 
     # -- 8-bit latent cache --------------------------------------------------------------------------------

@@ -18,7 +18,6 @@ def decoder():
     d.cfg, d.groups, d.num_pages, d.max_pages = CFG, CFG.g, 4, 4
     d.shape = d.shape_gqa = H.B.make_shape(CFG.B, CFG.h_q, CFG.g, CFG.d_h, CFG.r_kv, CFG.d_r, CFG.s_q, H.B.GQLA_BF16)
     d.d_lens = d.d_table = d.expanded_pool = d.expanded_blocks_pool = torch.zeros(16, dtype=torch.int32)
-    d.ws_t = None
     return d
 
 
@@ -75,3 +74,18 @@ def test_parts_of_a_joint_buffer_are_not_copied(monkeypatch):
     decoder().append_expanded(1e4, *parts)
     assert [seen[0].k_c, seen[0].v, seen[0].k_r] == [x.data_ptr() for x in parts]
     assert seen[0].k_stride == seen[0].v_stride == seen[0].kr_stride == joint.stride(0)
+
+
+def test_every_attention_call_has_a_workspace_of_its_own(monkeypatch):
+    """A recorded call goes on using its workspace, and calls on two streams overlap: none is shared, and none kept and freed for a larger one."""
+    sizes, taken = iter([4096, 0, 4096, 8192]), []
+    empty = torch.empty
+    monkeypatch.setattr(H.torch, "empty", lambda *a, device=None, **kw: empty(*a, **kw))
+    monkeypatch.setattr(H.B, "gqla_attend_gqa_workspace_bytes", lambda *a: next(sizes))
+    monkeypatch.setattr(H.B, "gqla_attend_gqa_fp8_blocks", lambda *a: taken.append(a[-1]))
+    d = decoder()
+    for _ in range(4):
+        d.attend_gqa_blocks(torch.zeros((2, CFG.h_q, CFG.d_h), dtype=torch.bfloat16), torch.zeros((2, CFG.h_q, D_R), dtype=torch.bfloat16))
+    assert [0 if w is None else w.numel() for w in taken] == [4096, 0, 4096, 8192]
+    assert len({w.data_ptr() for w in taken if w is not None}) == 3
+    assert not any(torch.is_tensor(x) and x.dtype == torch.uint8 for x in vars(d).values())
