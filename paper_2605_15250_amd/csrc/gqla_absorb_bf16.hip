@@ -1621,10 +1621,8 @@ __global__ void __launch_bounds__(512) combine_project_bf16_kernel(CombineArgs a
 
 static hipError_t launch_decode_absorb_general(const DecodeArgs& a, hipStream_t s) {
   constexpr int kLds = kSlots * kTile * (512 + 64) * 2;  // tile ring
-  // once per process (function-local statics are initialised under a lock); an error is reported by every call
-  static const hipError_t attr =
-      hipFuncSetAttribute((const void*)decode_absorb_bf16_kernel<512, 64>, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
-  if (attr != hipSuccess) return attr;
+  static DynamicLds lds;
+  if (const hipError_t e = lds.allow((const void*)decode_absorb_bf16_kernel<512, 64>, kLds); e != hipSuccess) return e;
   const int row_blocks = (a.M + kRowsPerBlock - 1) / kRowsPerBlock;
   const int chunks_padded = (a.n_chunks + 7) / 8 * 8;
   decode_absorb_bf16_kernel<512, 64><<<chunks_padded * row_blocks, 256, kLds, s>>>(a, row_blocks);
@@ -1634,9 +1632,8 @@ static hipError_t launch_decode_absorb_general(const DecodeArgs& a, hipStream_t 
 template <bool FP8>
 static hipError_t launch_decode_absorb_rows32(const DecodeArgs& a, float c_scale, hipStream_t s) {
   constexpr int kLds = (FP8 ? 6 * kTile * (512 + 64 * 2) : 4 * kTile * (512 + 64) * 2) + 2 * 4096 + 512;  // tile ring, probabilities, row maxima
-  static const hipError_t attr =
-      hipFuncSetAttribute((const void*)decode_absorb_rows32_bf16_kernel<512, 64, FP8>, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
-  if (attr != hipSuccess) return attr;
+  static DynamicLds lds;
+  if (const hipError_t e = lds.allow((const void*)decode_absorb_rows32_bf16_kernel<512, 64, FP8>, kLds); e != hipSuccess) return e;
   const int row_blocks = (a.M + 31) / 32;
   const int chunks_padded = (a.n_chunks + 7) / 8 * 8;
   decode_absorb_rows32_bf16_kernel<512, 64, FP8><<<chunks_padded * row_blocks, 512, kLds, s>>>(a, row_blocks, c_scale);
@@ -1646,9 +1643,8 @@ static hipError_t launch_decode_absorb_rows32(const DecodeArgs& a, float c_scale
 template <bool FP8>
 static hipError_t launch_decode_absorb_shared(const DecodeArgs& a, float c_scale, hipStream_t s) {
   constexpr int kLds = kSlots * kTile * (512 * (FP8 ? 1 : 2) + 64 * 2) + 2 * 8192;  // tile ring + the double-buffered exchange (16 bits: all 160 KB)
-  static const hipError_t attr =
-      hipFuncSetAttribute((const void*)decode_absorb_shared_bf16_kernel<512, 64, FP8>, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
-  if (attr != hipSuccess) return attr;
+  static DynamicLds lds;
+  if (const hipError_t e = lds.allow((const void*)decode_absorb_shared_bf16_kernel<512, 64, FP8>, kLds); e != hipSuccess) return e;
   const int row_blocks = (a.M + kRowsPerBlock - 1) / kRowsPerBlock;
   const int chunks_padded = (a.n_chunks + 7) / 8 * 8;
   decode_absorb_shared_bf16_kernel<512, 64, FP8><<<chunks_padded * row_blocks, 256, kLds, s>>>(a, row_blocks, c_scale);
@@ -1679,10 +1675,8 @@ hipError_t launch_decode_absorb_fp8(const DecodeArgs& a, float c_scale, hipStrea
 template <int DV, int PD>
 static hipError_t launch_combine_project_dims(const CombineArgs& a, int log2_rows, int n_blocks, hipStream_t s) {
   constexpr int kLds = 512 * PD * 2 + 32 * 1024;  // W_UV[j] and the exchange (128 dims: all 160 KB)
-  // once per process (function-local statics are initialised under a lock); an error is reported by every call
-  static const hipError_t attr =
-      hipFuncSetAttribute((const void*)combine_project_bf16_kernel<512, DV, PD>, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
-  if (attr != hipSuccess) return attr;
+  static DynamicLds lds;
+  if (const hipError_t e = lds.allow((const void*)combine_project_bf16_kernel<512, DV, PD>, kLds); e != hipSuccess) return e;
   const int per_group = 256 / (a.g * (DV / PD));  // workgroups per group: one per compute unit, each with its share of the blocks
   const int wgs = n_blocks < per_group || per_group < 1 ? n_blocks : per_group;
   const int grid = DV == PD ? wgs * a.g : (wgs * a.g + 7) / 8 * 8 * (DV / PD);

@@ -18,7 +18,6 @@
 // pipes busy 58 % of the cycles at the 1.85 GHz that the card holds meanwhile (a large product of bf16 matrices reaches 1.15).  9 to 16
 // tokens x 32 heads over 20000 to 32000, two sequences: 31 us and 6 of the merge, 14 stages in a row per workgroup.
 #include <algorithm>
-#include <atomic>
 #include <cmath>
 
 #include "gqla_lds.h"
@@ -451,20 +450,6 @@ __global__ void __launch_bounds__(256) attend_merge_kernel(AttendArgs a, int sli
   if (a.lse && v == 0) a.lse[at] = den == 0.f ? GQLA_NEG_INF : m + __logf(den);
 }
 
-// Dynamic LDS beyond 64 KB has to be allowed once per kernel and device.
-template <int DH, int DV>
-hipError_t allow_lds() {
-  static std::atomic<uint64_t> done{0};   // a bit per device
-  int dev = 0;
-  hipError_t e = hipGetDevice(&dev);
-  if (e != hipSuccess) return e;
-  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
-  if (done.load(std::memory_order_relaxed) & bit) return hipSuccess;
-  e = hipFuncSetAttribute((const void*)attend_kernel<DH, DV>, hipFuncAttributeMaxDynamicSharedMemorySize, AttendTile<DH, DV>::kLds);
-  if (e == hipSuccess) done.fetch_or(bit, std::memory_order_relaxed);
-  return e;
-}
-
 // tiles of rows of a sequence, if all have as many
 int64_t sequence_tiles(int64_t total, int64_t batch, int64_t G, int shift) {
   return std::max<int64_t>(1, (total * G + (batch << shift) - 1) / (batch << shift));
@@ -472,7 +457,8 @@ int64_t sequence_tiles(int64_t total, int64_t batch, int64_t G, int shift) {
 
 template <int DH, int DV>
 hipError_t launch_attend(const AttendArgs& a, hipStream_t s) {
-  hipError_t e = allow_lds<DH, DV>();
+  static DynamicLds lds;
+  hipError_t e = lds.allow((const void*)attend_kernel<DH, DV>, AttendTile<DH, DV>::kLds);
   if (e != hipSuccess) return e;
   const int64_t tiles = row_runs(a.total, a.G, a.tile_shift, 1, a.B), units = tiles * a.splits;
   // (spread: 64 sequences of 2500 to 5000 tokens, 8 groups, 4 to 8 rows of 4 heads each: 138 -> 123 us; 32 of 4000 to 6000, 4 rows of 16: 101 -> 93)

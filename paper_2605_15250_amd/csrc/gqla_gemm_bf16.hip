@@ -1035,9 +1035,8 @@ constexpr int kMaxWorkgroups = 8 * 256;
 
 template <int DH, int DV>
 static hipError_t launch_compress_dims(const CompressArgs& a, hipStream_t s) {
-  static const hipError_t attr =
-      hipFuncSetAttribute((const void*)compress_bf16_kernel<DH, DV, 512, 64>, hipFuncAttributeMaxDynamicSharedMemorySize, kCompressLds);
-  if (attr != hipSuccess) return attr;
+  static DynamicLds lds;
+  if (const hipError_t e = lds.allow((const void*)compress_bf16_kernel<DH, DV, 512, 64>, kCompressLds); e != hipSuccess) return e;
   // as many workgroups as tiles that the rows of the page table could hold, and enough for the shares of a few
   const int64_t blocks = ((int64_t)a.max_tokens + kCompressTok - 1) / kCompressTok * a.B;
   const int64_t grid = std::max(std::min<int64_t>(blocks, kMaxWorkgroups), std::min<int64_t>(4 * blocks, 256));
@@ -1052,9 +1051,8 @@ hipError_t launch_compress_bf16(const CompressArgs& a, hipStream_t s) {
 template <int SHARES>
 static hipError_t launch_absorb_query_staged(const AbsorbQueryArgs& a, int rows_per_group, int grid_x, hipStream_t s) {
   constexpr int kRows = 512 / SHARES, kLds = kRows * 128 * 2 + 4 * 32 * ((kRows >= 256 ? 128 : 64) + 16);  // the share of W_UK[j], output tiles
-  static const hipError_t attr = hipFuncSetAttribute((const void*)absorb_query_staged_bf16_kernel<512, SHARES>,
-                                                     hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
-  if (attr != hipSuccess) return attr;
+  static DynamicLds lds;
+  if (const hipError_t e = lds.allow((const void*)absorb_query_staged_bf16_kernel<512, SHARES>, kLds); e != hipSuccess) return e;
   absorb_query_staged_bf16_kernel<512, SHARES><<<dim3(grid_x, SHARES, a.g), 256, kLds, s>>>(a, rows_per_group);
   return hipGetLastError();
 }
@@ -1119,10 +1117,8 @@ hipError_t launch_expand_tail_fp8(const ExpandArgs& a, void* ws, hipStream_t s) 
 template <int DH, int DV, bool FP8, bool DIRECT>
 static hipError_t launch_expand_kernel(const ExpandArgs& a, const void* ws, unsigned grid, hipStream_t s) {
   constexpr int kLds = 2 * (512 / 16) * 2 * 1024;
-  // once per process (function-local statics are initialised under a lock); an error is reported by every call
-  static const hipError_t attr =
-      hipFuncSetAttribute((const void*)expand_bf16_kernel<DH, DV, 512, 64, FP8, DIRECT>, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
-  if (attr != hipSuccess) return attr;
+  static DynamicLds lds;
+  if (const hipError_t e = lds.allow((const void*)expand_bf16_kernel<DH, DV, 512, 64, FP8, DIRECT>, kLds); e != hipSuccess) return e;
   expand_bf16_kernel<DH, DV, 512, 64, FP8, DIRECT><<<grid, 256, kLds, s>>>(a, (const __bf16*)ws);
   return hipGetLastError();
 }

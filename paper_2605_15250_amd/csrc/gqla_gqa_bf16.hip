@@ -836,9 +836,8 @@ static hipError_t launch_decode_gqa_128(const DecodeArgs& a, float k_scale, floa
   if (a.G * a.s_q > 32) {  // more than one row block per group: two per wave, four waves per workgroup
     gqa_launch_shape(a, 4, 64, row_blocks, n_items, team, wpb, blocks);
     constexpr int kQBytesPerWave = 2 * (128 / 16 + 64 / 16) * 1024;  // both row blocks' query fragments
-    static const hipError_t attr = hipFuncSetAttribute((const void*)decode_gqa_bf16_kernel<128, 128, 64, FP8, 256, 2, false, false, BLK>,
-                                                       hipFuncAttributeMaxDynamicSharedMemorySize, 4 * kQBytesPerWave);
-    if (attr != hipSuccess) return attr;
+    static DynamicLds lds;
+    if (const hipError_t e = lds.allow((const void*)decode_gqa_bf16_kernel<128, 128, 64, FP8, 256, 2, false, false, BLK>, 4 * kQBytesPerWave); e != hipSuccess) return e;
     decode_gqa_bf16_kernel<128, 128, 64, FP8, 256, 2, false, false, BLK><<<blocks, 64 * wpb, wpb * kQBytesPerWave, s>>>(a, n_items, row_blocks, team ? 1 : 0,
                                                                                                     1, k_scale, v_scale);
     return hipGetLastError();
@@ -847,9 +846,8 @@ static hipError_t launch_decode_gqa_128(const DecodeArgs& a, float k_scale, floa
   // one group: the plan cuts chunks for teams of eight
   const int tt = a.g == 1 ? 8 : gqa_token_team_size(a, n_items, 8);
   if (tt > 1) {
-    static const hipError_t attr = hipFuncSetAttribute((const void*)decode_gqa_bf16_kernel<128, 128, 64, FP8, 512, 1, true, false, BLK>,
-                                                       hipFuncAttributeMaxDynamicSharedMemorySize, gqa_merge_bytes<128, BLK>(8));
-    if (attr != hipSuccess) return attr;
+    static DynamicLds lds;
+    if (const hipError_t e = lds.allow((const void*)decode_gqa_bf16_kernel<128, 128, 64, FP8, 512, 1, true, false, BLK>, gqa_merge_bytes<128, BLK>(8)); e != hipSuccess) return e;
     const int w = gqa_team_waves(a, n_items, tt, 8);
     decode_gqa_bf16_kernel<128, 128, 64, FP8, 512, 1, true, false, BLK><<<(n_items * tt + w - 1) / w, 64 * w, gqa_merge_bytes<128, BLK>(w), s>>>(a, n_items, row_blocks, 0, tt,
                                                                                                                          k_scale, v_scale);
@@ -877,9 +875,8 @@ static hipError_t launch_decode_gqa_192(const DecodeArgs& a, hipStream_t s) {
   gqa_launch_shape(a, 4, 32, row_blocks, n_items, team, wpb, blocks);
   const int tt = gqa_token_team_size(a, n_items, 4);
   if (tt > 1) {
-    static const hipError_t attr = hipFuncSetAttribute((const void*)decode_gqa_bf16_kernel<192, 256, 64, BLK, 256, 1, true, false, BLK>,
-                                                       hipFuncAttributeMaxDynamicSharedMemorySize, gqa_merge_bytes<256, BLK>(4));
-    if (attr != hipSuccess) return attr;
+    static DynamicLds lds;
+    if (const hipError_t e = lds.allow((const void*)decode_gqa_bf16_kernel<192, 256, 64, BLK, 256, 1, true, false, BLK>, gqa_merge_bytes<256, BLK>(4)); e != hipSuccess) return e;
     const int w = gqa_team_waves(a, n_items, tt, 4);
     decode_gqa_bf16_kernel<192, 256, 64, BLK, 256, 1, true, false, BLK><<<(n_items * tt + w - 1) / w, 64 * w, gqa_merge_bytes<256, BLK>(w), s>>>(a, n_items, row_blocks, 0, tt, 1.f, 1.f);
     return hipGetLastError();

@@ -3,11 +3,30 @@
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include <atomic>
 #include <vector>
 
 #include "gqla.h"
 
 namespace gqla {
+
+// Dynamic LDS beyond 64 KB has to be allowed once per kernel and device: one static object of this per kernel.
+class DynamicLds {
+ public:
+  hipError_t allow(const void* kernel, int bytes) {
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    const uint64_t bit = dev < 64 ? 1ull << dev : 0;   // (devices behind the 64th: with every call)
+    if (done_.load(std::memory_order_relaxed) & bit) return hipSuccess;
+    e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == hipSuccess) done_.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+  }
+
+ private:
+  std::atomic<uint64_t> done_{0};   // a bit per device
+};
 
 // One row of the chunk table that a decode kernel reads (16 bytes).
 struct ChunkEntry {

@@ -322,20 +322,18 @@ int out_proj_split(int M, int K, int D, int rows, int* krange) {
 }
 
 hipError_t launch_out_proj_bf16(const OutProjArgs& a, hipStream_t s) {
-  static const hipError_t attr = [] {
-    const hipError_t e2 = hipFuncSetAttribute((const void*)out_proj_bf16_kernel<2>, hipFuncAttributeMaxDynamicSharedMemorySize, out_proj_lds<2>());
-    const hipError_t e4 = hipFuncSetAttribute((const void*)out_proj_bf16_kernel<4>, hipFuncAttributeMaxDynamicSharedMemorySize, out_proj_lds<4>());
-    const hipError_t e8 = hipFuncSetAttribute((const void*)out_proj_bf16_kernel<8>, hipFuncAttributeMaxDynamicSharedMemorySize, out_proj_lds<8>());
-    return e2 != hipSuccess ? e2 : e4 != hipSuccess ? e4 : e8;
-  }();
-  if (attr != hipSuccess) return attr;
+  static DynamicLds lds2, lds4, lds8;
+  hipError_t e = a.rows == 64    ? lds2.allow((const void*)out_proj_bf16_kernel<2>, out_proj_lds<2>())
+                 : a.rows == 128 ? lds4.allow((const void*)out_proj_bf16_kernel<4>, out_proj_lds<4>())
+                                 : lds8.allow((const void*)out_proj_bf16_kernel<8>, out_proj_lds<8>());
+  if (e != hipSuccess) return e;
   // the kernel's per-lane byte offsets (row inside the tile times the row stride) are 32-bit
   if (a.K > (1 << 24) || a.krange % kOsK) return hipErrorInvalidValue;
   const dim3 grid(a.D / kOpN * a.ksplit * ((a.M + a.rows - 1) / a.rows));
   if (a.rows == 64) out_proj_bf16_kernel<2><<<grid, 64 * out_proj_waves<2>(), out_proj_lds<2>(), s>>>(a);
   else if (a.rows == 128) out_proj_bf16_kernel<4><<<grid, 64 * out_proj_waves<4>(), out_proj_lds<4>(), s>>>(a);
   else out_proj_bf16_kernel<8><<<grid, 64 * out_proj_waves<8>(), out_proj_lds<8>(), s>>>(a);
-  hipError_t e = hipGetLastError();
+  e = hipGetLastError();
   if (e != hipSuccess || a.ksplit == 1) return e;
   const int64_t total = (int64_t)a.M * a.D / 4;
   out_proj_reduce_kernel<<<(unsigned)((total + 255) / 256), 256, 0, s>>>(a);
