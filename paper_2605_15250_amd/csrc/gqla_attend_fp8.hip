@@ -14,9 +14,10 @@
 // The cache's vectors are operand fragments; a stage in LDS is a row of 1 KB pieces, one per fragment, so that a request writes and a
 // read takes 64 consecutive vectors (no bank is met twice).
 // Few rows over a long context: the tokens are split into ranges, whose partial outputs a second kernel joins.
-// Bound by the matrix cores on whole prompts: two of 2500 to 4000 tokens behind up to 500 x 128 heads 1085 to 1114 us = 1.06 to 1.09 PFLOP/s,
-// pipes busy 58 % of the cycles at the 1.85 GHz that the card holds meanwhile (a large product of bf16 matrices reaches 1.15).  9 to 16
-// tokens x 32 heads over 20000 to 32000, two sequences: 31 us and 6 of the merge, 14 stages in a row per workgroup.
+// Bound by the matrix cores on whole prompts: two of 2500 to 4000 tokens behind up to 500 x 128 heads 1108 to 1171 us = 1.01 to 1.07 PFLOP/s on
+// different cards, pipes busy 55 % of the cycles (a large product of bf16 matrices reaches 1.15).  9 to 16 tokens x 32 heads over 20000 to
+// 32000, two sequences: 31 us and 6 of the merge, 14 stages in a row per workgroup.  (Times further down that compare two forms were
+// taken ahead of the second sum, which adds 3 % to whole prompts, 1 to 2 % to the rest.)
 #include <algorithm>
 #include <cmath>
 
@@ -478,7 +479,7 @@ hipError_t launch_attend(const AttendArgs& a, hipStream_t s) {
 }  // namespace
 
 // Rows of a tile (2^7, or 2^6 for which two teams of waves share the tokens) and ranges that the tokens are split into: the pair with
-// the smallest time by this model, in microseconds, of the 256 units:
+// the smallest time by this model, in microseconds, of the 256 units, for sequences that all have max_tokens (the lengths are on the device):
 //   N = groups * tiles * splits workgroups of ceil(stages / splits) stages each (2.5 more for their start and end);
 //   a stage takes the k workgroups that share a unit stage[k] together.  k goes up to 3 (2 with value dims of 256);
 //   up to N = 256 k the workgroups with the most tokens in sight end last, beyond that a unit has N / (256 k) turns of the mean number
