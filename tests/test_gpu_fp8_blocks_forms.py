@@ -1,5 +1,6 @@
 """The forms that the decode over block scales takes where no chunk is shared out among waves, each with odd and even numbers of tiles,
-sequences that end early and a page that is not there; and the rotation of many heads, two tokens a workgroup, far out."""
+sequences that end early and a page that is not there; the rotation of many heads, two tokens a workgroup, far out; the calls without a
+page table or row bounds, and in tables far longer than the sequences."""
 import numpy as np
 import pytest
 import torch
@@ -107,3 +108,49 @@ def test_rotation_of_many_heads_far_out(g, G, d_h, d_v, blocks):
     got = held[table[seq, pos // P], :, pos % P].reshape(total, D_R)
     want = O.rope(kr, pos, BASE)
     assert np.all(np.abs(got - want) <= EPS * np.abs(want) + 2.0 ** -20 * 8)
+
+
+@pytest.mark.parametrize("g,G,d_h,d_v,P", [(2, 4, 128, 128, 64), (8, 16, 128, 128, 1024), (5, 4, 192, 256, 128)])
+def test_without_a_page_table_and_without_row_bounds(g, G, d_h, d_v, P):
+    """Sequence b's pages are b max_pages ..; every sequence has s_q rows: appended, attended as a chunk and decoded, in a cache whose rows of pages
+    are longer than the sequences."""
+    lens = [300, 2, 129]
+    w = World([n + 2 for n in lens], g, d_h, d_v, G=G, P=P, seed=231 + g, s_q=2, table=False)
+    w.append(lens)
+    _, q_rot, first, _ = w.append([2, 2, 2], uniform=True)
+    w.check_pool()
+    w.spoil()
+    q_c = stored(w.r.normal(size=(6, g * G, d_h)))
+    out, lse = decode(w, q_c, q_rot, units=256)
+    w.check_attention(out, lse, q_c, q_rot, first, w.lens())
+    out = torch.full((6, g * G, d_v), 7.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((6, g * G), 7.0, device="cuda")
+    need = B.gqla_attend_gqa_workspace_bytes(w.shape, None, 6, w.cache())
+    ws = torch.full((max(need, 16),), 0xFF, dtype=torch.uint8, device="cuda")
+    B.gqla_attend_gqa_fp8_blocks(w.shape, None, 6, bf16(q_c).cuda(), bf16(q_rot).cuda(), w.cache(), out, lse, ws)
+    torch.cuda.synchronize()
+    w.check_attention(out.float().cpu().numpy(), lse.cpu().numpy(), q_c, q_rot, first, w.lens())
+
+
+@pytest.mark.parametrize("g,G,d_h,d_v", [(8, 4, 128, 128), (4, 5, 192, 256)])
+def test_attention_in_tables_far_longer_than_the_sequences(g, G, d_h, d_v):
+    """Ranges for contexts that no sequence has: most see nothing, and the joined result is the one without them."""
+    lens, ns = [150, 1, 97, 200], [150, 1, 60, 130]
+    w = World(lens, g, d_h, d_v, G=G, seed=241 + g)
+    w.append(lens)
+    w.spoil()
+    table = np.full((w.B, 2048), w.pages + 7, np.int32)   # 131072 tokens; entries behind a sequence name no page
+    table[:, :w.max_pages] = w.table
+    wide = torch.from_numpy(table).cuda()
+    q_c, q_r = stored(w.r.normal(size=(sum(ns), g * G, d_h))), stored(w.r.normal(size=(sum(ns), g * G, D_R)))
+    first = np.concatenate([[0], np.cumsum(ns)]).astype(np.int32)
+    d_first = torch.from_numpy(first).cuda()
+    cache = B.make_cache(w.pool, w.d_lens, wide, w.P, 2048, w.pages, g)
+    need = B.gqla_attend_gqa_workspace_bytes(w.shape, d_first, sum(ns), cache)
+    assert need > B.gqla_attend_gqa_workspace_bytes(w.shape, d_first, sum(ns), w.cache())
+    ws = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")
+    out = torch.full((sum(ns), g * G, d_v), 7.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((sum(ns), g * G), 7.0, device="cuda")
+    B.gqla_attend_gqa_fp8_blocks(w.shape, d_first, sum(ns), bf16(q_c).cuda(), bf16(q_r).cuda(), cache, out, lse, ws)
+    torch.cuda.synchronize()
+    w.check_attention(out.float().cpu().numpy(), lse.cpu().numpy(), q_c, q_r, first, lens)
